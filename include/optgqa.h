@@ -494,6 +494,87 @@ int optgqa_prefill_step(void *out, const void *q, const void *k_new, const void 
                         int64_t v_token_stride, int dtype, void *stream);
 
 /*
+ * Rotary positions.  Of every head of q [num_tokens][num_heads][head_dim] and k [..][num_kv_heads][..] the first
+ * rotary_dim dims are pairs, pair i being the dims (i, i + rotary_dim / 2), or with interleaved != 0 the dims (2i, 2i + 1);
+ * the token at positions[t] turns pair (x, y) by the angle a = positions[t] * freqs[i] (radians):
+ *     x' = magnitude * (x cos a - y sin a),   y' = magnitude * (y cos a + x sin a)
+ * and the other dims pass through bit for bit.  The angle's product and its remainder modulo a turn are taken in 64 bits, the
+ * rest in 32, rounded once (nearest-even) to dtype.  backward != 0: the transpose, which is the gradient with respect to
+ * the rows given that of the turned rows (and, with magnitude 1, the inverse).
+ *
+ *   q, q_out        token t's rows start at element t * q_stride (q_out_stride); strides >= num_heads * head_dim: slices of a
+ *                   projection's rows will do.  q_out may be q with the same stride; other overlaps are undefined
+ *   k, k_out        likewise, num_kv_heads heads; num_kv_heads == 0 (or num_heads == 0): no such rows, NULL pointers
+ *   positions       [num_tokens] int32, any sign
+ *   freqs           [rotary_dim / 2] fp64, device (optgqa_rotary_frequencies_host makes them)
+ *   rotary_dim      even, 2 .. head_dim
+ *   magnitude       finite
+ * Fastest where pointers lie on 16 bytes, strides are multiples of 8 and rotary_dim of 16; anything else that is aligned
+ * to its elements works.  num_tokens == 0 does nothing.
+ */
+int optgqa_rotary_embedding(void *q_out, const void *q, void *k_out, const void *k,
+                            const int32_t *positions, const double *freqs, int num_tokens,
+                            int num_heads, int num_kv_heads, int head_dim, int rotary_dim,
+                            int interleaved, float magnitude, int backward, int64_t q_out_stride,
+                            int64_t q_stride, int64_t k_out_stride, int64_t k_stride, int dtype,
+                            void *stream);
+
+/*
+ * Cache append with the rotation on the way: optgqa_rotary_embedding of q into q_out, the turned rows of k and the rows of
+ * v stored as optgqa_reshape_and_cache stores them, in one launch and one pass over the data: the bits of those two calls.  Keys
+ * in the cache carry their positions; the attention calls then take NULL slopes.
+ *   slot_mapping    [num_tokens] int64; negative: k and v of that token are neither read nor stored (q is turned)
+ *   v               token stride v_stride >= num_kv_heads * head_dim
+ * The 8-bit calls store E4M3 codes, code = nearest_e4m3(fp32 turned value * fp32(1 / k_scale)): one rounding, of the turned
+ * value in 32 bits (and of v as optgqa_reshape_and_cache_fp8 rounds it); scales as for the optgqa_reshape_and_cache_fp8
+ * calls.
+ */
+int optgqa_rotary_and_cache(void *q_out, const void *q, const void *k, const void *v, void *k_cache,
+                            void *v_cache, const int64_t *slot_mapping, const int32_t *positions,
+                            const double *freqs, int num_tokens, int num_heads, int num_kv_heads,
+                            int head_dim, int rotary_dim, int interleaved, float magnitude,
+                            int block_size, int64_t q_out_stride, int64_t q_stride,
+                            int64_t k_stride, int64_t v_stride, int dtype, void *stream);
+
+int optgqa_rotary_and_cache_fp8(void *q_out, const void *q, const void *k, const void *v,
+                                void *k_cache, void *v_cache, const int64_t *slot_mapping,
+                                const int32_t *positions, const double *freqs, int num_tokens,
+                                int num_heads, int num_kv_heads, int head_dim, int rotary_dim,
+                                int interleaved, float magnitude, int block_size,
+                                int64_t q_out_stride, int64_t q_stride, int64_t k_stride,
+                                int64_t v_stride, float k_scale, float v_scale, int dtype,
+                                void *stream);
+
+int optgqa_rotary_and_cache_fp8_heads(void *q_out, const void *q, const void *k, const void *v,
+                                      void *k_cache, void *v_cache, const int64_t *slot_mapping,
+                                      const int32_t *positions, const double *freqs, int num_tokens,
+                                      int num_heads, int num_kv_heads, int head_dim, int rotary_dim,
+                                      int interleaved, float magnitude, int block_size,
+                                      int64_t q_out_stride, int64_t q_stride, int64_t k_stride,
+                                      int64_t v_stride, const float *k_scales,
+                                      const float *v_scales, int dtype, void *stream);
+
+/*
+ * Frequencies for the calls above, on the host: freqs_host[i] = base^(-2i / rotary_dim) in 64 bits (base > 1), changed for
+ * contexts beyond the ones a model was trained on by `scaling`:
+ *   OPTGQA_ROTARY_PLAIN       not at all
+ *   OPTGQA_ROTARY_LINEAR      divided by `factor` (>= 1)
+ *   OPTGQA_ROTARY_BASE        base becomes base * factor^(rotary_dim / (rotary_dim - 2))
+ *   OPTGQA_ROTARY_YARN        pairs that make more than a turns over original_len tokens are kept, those that make less than b
+ *                             divided by factor, a ramp over the pairs between (usual: a = 32, b = 1); magnitude 0.1 ln(factor) + 1
+ *   OPTGQA_ROTARY_WAVELENGTH  pairs that make more than b turns over original_len are kept, those with less than a divided by
+ *                             factor, interpolated by their turns between (usual: a = 1, b = 4)
+ * *magnitude_host: 1 but for YARN.  Arguments that a scaling does not use are not looked at.
+ */
+typedef enum {
+    OPTGQA_ROTARY_PLAIN = 0, OPTGQA_ROTARY_LINEAR = 1, OPTGQA_ROTARY_BASE = 2, OPTGQA_ROTARY_YARN = 3,
+    OPTGQA_ROTARY_WAVELENGTH = 4
+} optgqa_rotary_scaling;
+int optgqa_rotary_frequencies_host(double *freqs_host, float *magnitude_host, int rotary_dim,
+                                   double base, int scaling, double factor, double original_len,
+                                   double a, double b);
+
+/*
  * Diagnostic: un-page the cache (Section III-A: pages are only a re-arrangement of the
  * sequence).  k_out / v_out are [num_seqs][max_context_len][num_kv_heads][head_dim]; token j of
  * sequence b is copied bit for bit for j < context_lens[b]; other rows are left untouched.

@@ -123,6 +123,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.optgqa_gather_kv.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp]
     lib.optgqa_validate_tables_host.restype = i32
     lib.optgqa_validate_tables_host.argtypes = [vp, vp, i32, i32, i32, i32]
+    operators.declare(lib)
     _lib = lib
     return lib
 
@@ -192,14 +193,15 @@ def _workspace(ws: Optional[torch.Tensor], ref: torch.Tensor) -> int:
     return ws.numel() * ws.element_size()
 
 
-def _typed(ref: torch.Tensor, *, same=(), u8=(), i32=(), i64=(), f32=()) -> None:
+def _typed(ref: torch.Tensor, *, same=(), u8=(), i32=(), i64=(), f32=(), f64=()) -> None:
     """Refuse, before any pointer is taken, what the C ABI cannot check: the library reads raw
     device pointers, so a tensor of another element type or on another device would be misread
     (block ids and slots out of range make the kernels write out of bounds).  ``ref`` (q, or k for
     the cache writes) fixes the 2-byte type and the device; each group is a list of (name, tensor
     or None).  Element types first (TypeError), then devices (ValueError)."""
     _dtype_code(ref)
-    groups = ((same, ref.dtype), (u8, torch.uint8), (i32, torch.int32), (i64, torch.int64), (f32, torch.float32))
+    groups = ((same, ref.dtype), (u8, torch.uint8), (i32, torch.int32), (i64, torch.int64), (f32, torch.float32),
+              (f64, torch.float64))
     for group, want in groups:
         for name, t in group:
             if t is None:
@@ -813,3 +815,10 @@ def validate_tables_host(block_tables, context_lens, block_size: int, num_blocks
     return int(lib.optgqa_validate_tables_host(bt.ctypes.data_as(ctypes.c_void_p),
                                                cl.ctypes.data_as(ctypes.c_void_p), int(cl.shape[0]),
                                                int(bt.shape[1]), int(block_size), int(num_blocks)))
+
+
+from . import operators  # noqa: E402  (uses the helpers above)
+from .operators import (  # noqa: E402, F401
+    ROTARY_BASE, ROTARY_LINEAR, ROTARY_PLAIN, ROTARY_WAVELENGTH, ROTARY_YARN, rotary_and_cache, rotary_and_cache_fp8,
+    rotary_and_cache_fp8_heads, rotary_embedding, rotary_frequencies,
+)

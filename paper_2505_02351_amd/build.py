@@ -14,7 +14,8 @@ import sys
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
-SRC = os.path.join(PKG, "csrc", "optgqa.hip")
+SRC = os.path.join(PKG, "csrc", "liboptgqa.hip")          # all of it in one file
+PARTS = ("optgqa.hip", "operators.hip")                   # what SRC includes, compiled side by side
 LIB = os.path.join(PKG, "liboptgqa.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 
@@ -26,23 +27,36 @@ HIPCC_FLAGS = [
 
 
 def build(keep_asm: bool = False, verbose: bool = False, defines=(), out: str = LIB) -> str:
-    """Compile csrc/optgqa.hip.  `defines` (e.g. ["OPTGQA_RING_TILES=4"]) and `out` exist for
+    """Compile csrc/*.hip.  `defines` (e.g. ["OPTGQA_RING_TILES=4"]) and `out` exist for
     tuning experiments; the product library is the default call."""
     os.makedirs(BUILD_DIR, exist_ok=True)
     tmp = os.path.join(BUILD_DIR, f"liboptgqa.{os.getpid()}.so")
-    cmd = ["hipcc", *HIPCC_FLAGS, *["-D" + d for d in defines], "-I" + os.path.join(ROOT, "include"),
-           "-I" + os.path.join(PKG, "csrc"), SRC, "-o", tmp]
-    if keep_asm:
-        cmd.append("-save-temps=obj")
-    res = subprocess.run(cmd, capture_output=True, text=True, cwd=BUILD_DIR)
-    noise = "'-packed-fp32-ops' is not a recognized feature"       # host pass does not know the feature
-    err = "\n".join(l for l in res.stderr.splitlines() if noise not in l)
-    if res.returncode != 0:
-        raise RuntimeError(f"hipcc failed ({res.returncode}):\n{err}")
-    if verbose and err.strip():
-        print(err, file=sys.stderr)
+    objects = [os.path.join(BUILD_DIR, f"{os.path.splitext(p)[0]}.{os.getpid()}.o") for p in PARTS]
+    flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+    cmds = [["hipcc", *flags, "-c", *["-D" + d for d in defines], "-I" + os.path.join(ROOT, "include"), "-I" + os.path.join(PKG, "csrc"),
+             *(["-save-temps=obj"] if keep_asm else []), os.path.join(PKG, "csrc", p), "-o", o] for p, o in zip(PARTS, objects)]
+    try:
+        running = [subprocess.Popen(c, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, cwd=BUILD_DIR) for c in cmds]
+        said = [r.communicate()[0] for r in running]             # (all are waited for before any is judged)
+        for r, text in zip(running, said):
+            _judge(r.returncode, text, verbose)
+        res = subprocess.run(["hipcc", *HIPCC_FLAGS, *objects, "-o", tmp], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, cwd=BUILD_DIR)
+        _judge(res.returncode, res.stdout, verbose)
+    finally:
+        for o in objects:
+            if os.path.exists(o):
+                os.remove(o)
     os.replace(tmp, out)
     return out
+
+
+def _judge(status: int, text: str, verbose: bool) -> None:
+    noise = "'-packed-fp32-ops' is not a recognized feature"       # host pass does not know the feature
+    err = "\n".join(l for l in text.splitlines() if noise not in l)
+    if status != 0:
+        raise RuntimeError(f"hipcc failed ({status}):\n{err}")
+    if verbose and err.strip():
+        print(err, file=sys.stderr)
 
 
 if __name__ == "__main__":

@@ -1,0 +1,233 @@
+// C ABI of what stands around the attention of a step: rotary positions, rotated cache appends.
+// Declarations and the meaning of every argument: include/optgqa.h.
+#include "optgqa.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "host.hpp"
+#include "rotary_kernels.hpp"
+
+using namespace optgqa;
+
+namespace {
+
+// What the rotary entry points are called with.
+struct RotaryCall {
+    void* q_out;
+    const void* q;
+    void* k_out;
+    const void *k, *v;
+    void *k_cache, *v_cache;
+    const int64_t* slots;
+    const int32_t* positions;
+    const double* freqs;
+    int num_tokens, num_heads, num_kv_heads, head_dim, rotary_dim, interleaved, block_size;
+    int64_t q_out_stride, q_stride, k_out_stride, k_stride, v_stride;
+    float magnitude;
+    bool backward;
+    const KvScales* scales;     // E4M3 caches
+    int dtype;
+};
+
+template <int DT, RotaryTo TO, bool INTERLEAVED>
+int launch_rotary_v(const RotaryParams& p, bool wide, dim3 grid, hipStream_t st)
+{
+    return wide ? launch(rotary_kernel<DT, TO, INTERLEAVED, 8>, grid, dim3(kRotaryThreads), 0, st, p)
+                : launch(rotary_kernel<DT, TO, INTERLEAVED, 1>, grid, dim3(kRotaryThreads), 0, st, p);
+}
+
+template <RotaryTo TO>
+int launch_rotary(const RotaryParams& p, int dtype, bool interleaved, bool wide, dim3 grid, hipStream_t st)
+{
+    if (dtype == OPTGQA_F16)
+        return interleaved ? launch_rotary_v<kF16, TO, true>(p, wide, grid, st) : launch_rotary_v<kF16, TO, false>(p, wide, grid, st);
+    return interleaved ? launch_rotary_v<kBF16, TO, true>(p, wide, grid, st) : launch_rotary_v<kBF16, TO, false>(p, wide, grid, st);
+}
+
+int rotary_impl(const RotaryCall& c, RotaryTo to, hipStream_t st)
+{
+    const bool store = to != RotaryTo::kRows;
+    if (c.num_tokens < 0 || c.num_heads < 0 || c.num_kv_heads < 0 || (store && (c.num_heads <= 0 || c.num_kv_heads <= 0)) ||
+        c.num_heads + (int64_t)c.num_kv_heads <= 0 || c.num_heads > 65535 || c.num_kv_heads > 65535)
+        return OPTGQA_ERR_SHAPE;
+    if (!dtype_ok(c.dtype) || !head_dim_ok(c.head_dim) || (store && !block_size_ok(c.block_size))) return OPTGQA_ERR_UNSUPPORTED;
+    if (c.rotary_dim <= 0 || c.rotary_dim > c.head_dim || c.rotary_dim % 2) return OPTGQA_ERR_SHAPE;
+    if (!std::isfinite(c.magnitude)) return OPTGQA_ERR_SHAPE;
+    if (to == RotaryTo::kCacheE4M3) {
+        if (c.scales->per_head() && !c.scales->v_heads) return OPTGQA_ERR_NULL;
+        if (!c.scales->valid()) return OPTGQA_ERR_SHAPE;
+    }
+    const int64_t q_row = (int64_t)c.num_heads * c.head_dim, kv_row = (int64_t)c.num_kv_heads * c.head_dim;
+    if (c.num_heads && (c.q_stride < q_row || c.q_out_stride < q_row)) return OPTGQA_ERR_SHAPE;
+    if (c.num_kv_heads && (c.k_stride < kv_row || (store ? c.v_stride < kv_row : c.k_out_stride < kv_row))) return OPTGQA_ERR_SHAPE;
+    if (c.num_tokens == 0) return OPTGQA_OK;
+    if (!c.positions || !c.freqs || (c.num_heads && (!c.q || !c.q_out)) || (c.num_kv_heads && !c.k)) return OPTGQA_ERR_NULL;
+    if (store ? !c.v || !c.k_cache || !c.v_cache || !c.slots : c.num_kv_heads && !c.k_out) return OPTGQA_ERR_NULL;
+
+    // (what a call does not have is a null pointer or a zero stride here, and on any alignment)
+    const uintptr_t rows = reinterpret_cast<uintptr_t>(c.q) | reinterpret_cast<uintptr_t>(c.q_out) | reinterpret_cast<uintptr_t>(c.k) |
+                           reinterpret_cast<uintptr_t>(c.k_out) | reinterpret_cast<uintptr_t>(c.v);
+    const uintptr_t caches = reinterpret_cast<uintptr_t>(c.k_cache) | reinterpret_cast<uintptr_t>(c.v_cache);
+    if ((rows & 1u) || (to == RotaryTo::kCache && (caches & 1u)) || (reinterpret_cast<uintptr_t>(c.freqs) & 7u) ||
+        (reinterpret_cast<uintptr_t>(c.positions) & 3u))
+        return OPTGQA_ERR_UNSUPPORTED;
+    const bool wide = !(rows & 15u) && !(caches & (to == RotaryTo::kCacheE4M3 ? 7u : 15u)) && c.rotary_dim % 16 == 0 &&
+                      (c.q_stride | c.q_out_stride | c.k_stride | c.k_out_stride | c.v_stride) % 8 == 0;
+
+    RotaryParams p;
+    p.q = c.q;
+    p.q_out = c.q_out;
+    p.k = c.k;
+    p.k_out = c.k_out;
+    p.v = c.v;
+    p.k_cache = c.k_cache;
+    p.v_cache = c.v_cache;
+    p.slots = c.slots;
+    p.positions = c.positions;
+    p.freqs = c.freqs;
+    p.q_stride = c.q_stride;
+    p.q_out_stride = c.q_out_stride;
+    p.k_stride = c.k_stride;
+    p.k_out_stride = c.k_out_stride;
+    p.v_stride = c.v_stride;
+    p.magnitude = c.magnitude;
+    p.sign = c.backward ? -1.f : 1.f;
+    p.k_inv_scale = p.v_inv_scale = 1.f;
+    p.k_scales = p.v_scales = nullptr;
+    if (to == RotaryTo::kCacheE4M3) {
+        p.k_scales = c.scales->k_heads;
+        p.v_scales = c.scales->v_heads;
+        if (!c.scales->per_head()) {
+            p.k_inv_scale = 1.0f / c.scales->k;
+            p.v_inv_scale = 1.0f / c.scales->v;
+        }
+    }
+    p.num_tokens = c.num_tokens;
+    p.q_heads = c.num_heads;
+    p.kv_heads = c.num_kv_heads;
+    p.heads = c.num_heads + c.num_kv_heads * (store ? 2 : 1);
+    p.pairs = c.rotary_dim / 2;
+    p.head_dim = c.head_dim;
+    p.pieces_shift = __builtin_ctz(c.head_dim / (wide ? 16 : 2));
+    p.block_shift = store ? __builtin_ctz(c.block_size) : 0;
+
+    // Many tokens: whole tokens, up to 8, some 1 500 items for a workgroup's 256 threads, so that a token's angles are worked
+    // out once.  Fewer than that makes four workgroups to a CU: one token each, its heads dealt to workgroups of one item a thread.
+    const int64_t per_token = (int64_t)p.heads << p.pieces_shift;
+    p.tokens_per_wg = (int)std::min<int64_t>(std::max<int64_t>(1536 / per_token, 1), kRotaryMaxTokens);
+    p.heads_per_wg = p.heads;
+    if (c.num_tokens < (int64_t)4 * num_cus() * p.tokens_per_wg) {
+        p.tokens_per_wg = 1;
+        p.heads_per_wg = std::min(p.heads, kRotaryThreads >> p.pieces_shift);
+    }
+    p.by_heads_per_wg.set((uint32_t)p.heads_per_wg);
+    p.by_pairs.set((uint32_t)p.pairs);
+    const dim3 grid((unsigned)(((int64_t)c.num_tokens + p.tokens_per_wg - 1) / p.tokens_per_wg),
+                    (unsigned)((p.heads + p.heads_per_wg - 1) / p.heads_per_wg));
+    if (to == RotaryTo::kRows) return launch_rotary<RotaryTo::kRows>(p, c.dtype, c.interleaved != 0, wide, grid, st);
+    if (to == RotaryTo::kCache) return launch_rotary<RotaryTo::kCache>(p, c.dtype, c.interleaved != 0, wide, grid, st);
+    return launch_rotary<RotaryTo::kCacheE4M3>(p, c.dtype, c.interleaved != 0, wide, grid, st);
+}
+
+int rotary_and_cache_impl(void* q_out, const void* q, const void* k, const void* v, void* k_cache, void* v_cache,
+                          const int64_t* slot_mapping, const int32_t* positions, const double* freqs, int num_tokens, int num_heads,
+                          int num_kv_heads, int head_dim, int rotary_dim, int interleaved, float magnitude, int block_size,
+                          int64_t q_out_stride, int64_t q_stride, int64_t k_stride, int64_t v_stride, const KvScales* scales, int dtype, void* stream)
+{
+    const RotaryCall c{q_out, q, nullptr, k, v, k_cache, v_cache, slot_mapping, positions, freqs, num_tokens, num_heads, num_kv_heads, head_dim,
+                       rotary_dim, interleaved, block_size, q_out_stride, q_stride, 0, k_stride, v_stride, magnitude, false, scales, dtype};
+    return rotary_impl(c, scales ? RotaryTo::kCacheE4M3 : RotaryTo::kCache, static_cast<hipStream_t>(stream));
+}
+
+}  // namespace
+
+extern "C" {
+
+int optgqa_rotary_frequencies_host(double* freqs_host, float* magnitude_host, int rotary_dim, double base, int scaling, double factor,
+                                   double original_len, double a, double b)
+{
+    if (!freqs_host || !magnitude_host) return OPTGQA_ERR_NULL;
+    if (rotary_dim <= 0 || rotary_dim % 2 || !(base > 1.0) || !std::isfinite(base)) return OPTGQA_ERR_SHAPE;
+    if (scaling < OPTGQA_ROTARY_PLAIN || scaling > OPTGQA_ROTARY_WAVELENGTH) return OPTGQA_ERR_UNSUPPORTED;
+    if (scaling != OPTGQA_ROTARY_PLAIN && !(factor >= 1.0 && std::isfinite(factor))) return OPTGQA_ERR_SHAPE;
+    const bool by_length = scaling == OPTGQA_ROTARY_YARN || scaling == OPTGQA_ROTARY_WAVELENGTH;
+    if (by_length && !(original_len > 0.0 && std::isfinite(original_len) && a > 0.0 && b > 0.0 && std::isfinite(a) && std::isfinite(b)))
+        return OPTGQA_ERR_SHAPE;
+    if (scaling == OPTGQA_ROTARY_YARN && !(a > b)) return OPTGQA_ERR_SHAPE;
+    if (scaling == OPTGQA_ROTARY_WAVELENGTH && !(b > a)) return OPTGQA_ERR_SHAPE;
+    if (scaling == OPTGQA_ROTARY_BASE && rotary_dim <= 2) return OPTGQA_ERR_SHAPE;
+    const double two_pi = 6.283185307179586476925;
+    const int pairs = rotary_dim / 2;
+    if (scaling == OPTGQA_ROTARY_BASE) base *= std::pow(factor, rotary_dim / (rotary_dim - 2.0));
+    // YaRN: the pair that makes `turns` turns over the original length
+    auto pair_of = [&](double turns) { return rotary_dim * std::log(original_len / (turns * two_pi)) / (2.0 * std::log(base)); };
+    double lo = 0.0, hi = 0.0;
+    if (scaling == OPTGQA_ROTARY_YARN) {
+        lo = std::max(std::floor(pair_of(a)), 0.0);
+        hi = std::min(std::ceil(pair_of(b)), rotary_dim - 1.0);
+    }
+    for (int i = 0; i < pairs; ++i) {
+        double f = std::pow(base, -2.0 * i / rotary_dim);
+        if (scaling == OPTGQA_ROTARY_LINEAR) f /= factor;
+        if (scaling == OPTGQA_ROTARY_YARN) {
+            const double ramp = std::min(std::max((i - lo) / std::max(hi - lo, 0.001), 0.0), 1.0);
+            f = f * (1.0 - ramp) + f / factor * ramp;
+        }
+        if (scaling == OPTGQA_ROTARY_WAVELENGTH) {
+            const double turns = original_len * f / two_pi;                  // over the original length
+            const double keep = std::min(std::max((turns - a) / (b - a), 0.0), 1.0);
+            f = f * keep + f / factor * (1.0 - keep);
+        }
+        freqs_host[i] = f;
+    }
+    *magnitude_host = scaling == OPTGQA_ROTARY_YARN ? (float)(0.1 * std::log(factor) + 1.0) : 1.f;
+    return OPTGQA_OK;
+}
+
+int optgqa_rotary_embedding(void* q_out, const void* q, void* k_out, const void* k, const int32_t* positions, const double* freqs,
+                            int num_tokens, int num_heads, int num_kv_heads, int head_dim, int rotary_dim, int interleaved,
+                            float magnitude, int backward, int64_t q_out_stride, int64_t q_stride, int64_t k_out_stride,
+                            int64_t k_stride, int dtype, void* stream)
+{
+    const RotaryCall c{q_out, q, k_out, k, nullptr, nullptr, nullptr, nullptr, positions, freqs, num_tokens, num_heads, num_kv_heads, head_dim,
+                       rotary_dim, interleaved, 16, q_out_stride, q_stride, k_out_stride, k_stride, 0, magnitude, backward != 0, nullptr, dtype};
+    return rotary_impl(c, RotaryTo::kRows, static_cast<hipStream_t>(stream));
+}
+
+int optgqa_rotary_and_cache(void* q_out, const void* q, const void* k, const void* v, void* k_cache, void* v_cache,
+                            const int64_t* slot_mapping, const int32_t* positions, const double* freqs, int num_tokens,
+                            int num_heads, int num_kv_heads, int head_dim, int rotary_dim, int interleaved, float magnitude,
+                            int block_size, int64_t q_out_stride, int64_t q_stride, int64_t k_stride, int64_t v_stride, int dtype,
+                            void* stream)
+{
+    return rotary_and_cache_impl(q_out, q, k, v, k_cache, v_cache, slot_mapping, positions, freqs, num_tokens, num_heads, num_kv_heads, head_dim,
+                                 rotary_dim, interleaved, magnitude, block_size, q_out_stride, q_stride, k_stride, v_stride, nullptr, dtype, stream);
+}
+
+int optgqa_rotary_and_cache_fp8(void* q_out, const void* q, const void* k, const void* v, void* k_cache, void* v_cache,
+                                const int64_t* slot_mapping, const int32_t* positions, const double* freqs, int num_tokens,
+                                int num_heads, int num_kv_heads, int head_dim, int rotary_dim, int interleaved, float magnitude,
+                                int block_size, int64_t q_out_stride, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                                float k_scale, float v_scale, int dtype, void* stream)
+{
+    const KvScales scales{k_scale, v_scale, nullptr, nullptr};
+    return rotary_and_cache_impl(q_out, q, k, v, k_cache, v_cache, slot_mapping, positions, freqs, num_tokens, num_heads, num_kv_heads, head_dim,
+                                 rotary_dim, interleaved, magnitude, block_size, q_out_stride, q_stride, k_stride, v_stride, &scales, dtype, stream);
+}
+
+int optgqa_rotary_and_cache_fp8_heads(void* q_out, const void* q, const void* k, const void* v, void* k_cache, void* v_cache,
+                                      const int64_t* slot_mapping, const int32_t* positions, const double* freqs, int num_tokens,
+                                      int num_heads, int num_kv_heads, int head_dim, int rotary_dim, int interleaved,
+                                      float magnitude, int block_size, int64_t q_out_stride, int64_t q_stride, int64_t k_stride,
+                                      int64_t v_stride, const float* k_scales, const float* v_scales, int dtype, void* stream)
+{
+    if (!k_scales || !v_scales) return OPTGQA_ERR_NULL;
+    const KvScales scales{0.f, 0.f, k_scales, v_scales};
+    return rotary_and_cache_impl(q_out, q, k, v, k_cache, v_cache, slot_mapping, positions, freqs, num_tokens, num_heads, num_kv_heads, head_dim,
+                                 rotary_dim, interleaved, magnitude, block_size, q_out_stride, q_stride, k_stride, v_stride, &scales, dtype, stream);
+}
+
+}  // extern "C"

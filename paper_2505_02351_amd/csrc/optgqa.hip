@@ -7,10 +7,9 @@
 #include <algorithm>
 #include <cmath>
 #include <mutex>
-#include <tuple>
 #include <type_traits>
-#include <utility>
 
+#include "host.hpp"
 #include "cache_kernels.hpp"
 #include "decode_kernels.hpp"
 #include "decode_mc_kernels.hpp"
@@ -34,25 +33,6 @@ namespace {
 constexpr int kAbiVersion = 2;
 constexpr int kMinPartition = 256;        // tokens; smaller runs are dominated by the merge
 
-bool dtype_ok(int dt) { return dt == OPTGQA_F16 || dt == OPTGQA_BF16; }
-bool head_dim_ok(int d) { return d == 64 || d == 128; }
-bool block_size_ok(int bs) { return bs == 16 || bs == 32 || bs == 64; }
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-// Launch through the call that reports THIS launch's own status (hipLaunchKernel): an error
-// some earlier work of the caller left behind in the runtime's "last error" slot is neither
-// reported as ours nor cleared.
-template <typename... KArgs, typename... Args>
-int launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t lds_bytes, hipStream_t st, Args&&... args)
-{
-    static_assert(sizeof...(KArgs) == sizeof...(Args), "argument count does not match the kernel");
-    std::tuple<std::decay_t<KArgs>...> vals(std::forward<Args>(args)...);
-    void* ptrs[sizeof...(KArgs)];
-    std::apply([&](auto&... v) { int i = 0; ((ptrs[i++] = static_cast<void*>(&v)), ...); }, vals);
-    return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, ptrs, lds_bytes, st) == hipSuccess
-               ? OPTGQA_OK : OPTGQA_ERR_LAUNCH;
-}
-
 // Cache store of 2-byte rows; wide: everything lies on 16 bytes and rows move as 16-byte pieces, else element by element.
 int launch_cache_store(const StoreRows& rows, bool wide, void* k_cache, void* v_cache, int num_tokens, int num_kv_heads, int head_dim,
                        int block_size, hipStream_t st)
@@ -63,20 +43,6 @@ int launch_cache_store(const StoreRows& rows, bool wide, void* k_cache, void* v_
         return launch(wide ? reshape_and_cache_kernel<uint4> : reshape_and_cache_kernel<uint16_t>, grid, dim3(256), 0, st, r.k, r.v, kc, vc,
                       r.slot_mapping, n, r.k_stride, r.v_stride, r.block_tables, r.context_lens, r.max_blocks_per_seq);
     });
-}
-
-// Compute units of the current device, asked once (every GPU of a box is the same part); 256,
-// the MI355X count, where no device answers (the sizing calls also work on a GPU-less host).
-int num_cus()
-{
-    static const int cus = [] {
-        int dev = 0, n = 0;
-        if (hipGetDevice(&dev) != hipSuccess ||
-            hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0)
-            return 256;
-        return n;
-    }();
-    return cus;
 }
 
 // Profiling aid (optgqa_set_kernel_events): events recorded around the launch of the kernel that
@@ -439,17 +405,6 @@ int launch_prefill_mma(const PrefillParams& p, int head_dim, dim3 grid, PrefillS
     return launch_prefill_d<DT, KV8, WIN, CONTIG, STEP, false, 128>(p, grid, shape, st);
 }
 
-// The tiled prefill kernel carries the tile-invariant part of the ALiBi term inside the score
-// accumulator as slope / scale, so it cannot take a score scale of exactly zero.  Magnitudes
-// below 2^-64 (zero included) are evaluated as +-2^-64: the scores then differ from the exact
-// ones by |q.k| * 2^-64, far below fp32 resolution of the bias they are added to.
-float prefill_scale2(float scale)
-{
-    const float tiny = 0x1p-64f;
-    const float s = std::fabs(scale) < tiny ? std::copysign(tiny, scale) : scale;
-    return s * kLog2e;
-}
-
 // Tiled matrix-core prefill (head_dim 128 or 64).
 int launch_prefill(PrefillParams p, int num_seqs, int max_q_len, int head_dim, int dtype, hipStream_t st,
                    bool kv8 = false, bool contig = false, bool step = false)
@@ -576,20 +531,6 @@ size_t optgqa_paged_attention_workspace_bytes(int num_seqs, int num_heads, int n
 }  // extern "C"
 
 namespace {
-
-// Scales of 8-bit (E4M3) caches: one pair per tensor (k, v), or - k_heads / v_heads set, device
-// arrays of num_kv_heads values each - one pair per KV head.
-struct KvScales {
-    float k, v;
-    const float* k_heads;
-    const float* v_heads;
-    bool per_head() const { return k_heads != nullptr; }
-    bool valid() const
-    {
-        if (per_head()) return v_heads != nullptr;           // contents live on the device: not checked here
-        return k > 0.f && v > 0.f && k <= 3e38f && v <= 3e38f;
-    }
-};
 
 // New-token inputs of a fused decode step (all null / zero for plain attention).
 struct StepInputs {

@@ -1,0 +1,110 @@
+"""Host-only checks of the operators around a step's attention: frequencies, sizes, and what is refused before any launch."""
+import ctypes
+import math
+import os
+
+import numpy as np
+import pytest
+
+
+@pytest.fixture(scope="module")
+def G():
+    import paper_2505_02351_amd as G
+    if not os.path.exists(G.LIB_PATH):
+        from paper_2505_02351_amd import build
+        build.build()
+    G.load_library()
+    return G
+
+
+ONE = ctypes.c_void_p(16)       # non-null, aligned, never dereferenced: every call below fails first or has nothing to do
+
+
+def test_rotary_frequencies(G):
+    f, m = G.rotary_frequencies(128, 10000.0)
+    assert m == 1.0 and np.allclose(f.numpy(), 10000.0 ** (-np.arange(0, 128, 2) / 128), rtol=1e-14, atol=0)
+    g, m = G.rotary_frequencies(128, 10000.0, G.ROTARY_LINEAR, 4.0)
+    assert m == 1.0 and np.allclose(g, f / 4, rtol=1e-14, atol=0)
+    g, m = G.rotary_frequencies(128, 10000.0, G.ROTARY_BASE, 4.0)     # the slowest pair is slowed by the factor, the fastest not at all
+    assert m == 1.0 and g[0] == 1.0 and math.isclose(g[63], f[63] / 4, rel_tol=1e-12) and (g[1:] < f[1:]).all()
+    g, m = G.rotary_frequencies(64, 10000.0, G.ROTARY_YARN, 16.0, 4096.0)
+    f, _ = G.rotary_frequencies(64, 10000.0)
+    turns = 4096.0 * f / (2 * math.pi)
+    assert math.isclose(m, 0.1 * math.log(16.0) + 1.0, rel_tol=1e-6)
+    assert (g[turns > 64] == f[turns > 64]).all() and np.allclose(g[turns < 0.5], f[turns < 0.5] / 16, rtol=1e-12, atol=0)
+    assert (g <= f).all() and (g >= f / 16.001).all() and (g[1:] < g[:-1]).all()
+    g, m = G.rotary_frequencies(64, 10000.0, G.ROTARY_WAVELENGTH, 8.0, 4096.0)
+    assert m == 1.0 and (g[turns >= 4] == f[turns >= 4]).all() and np.allclose(g[turns <= 1], f[turns <= 1] / 8, rtol=1e-12, atol=0)
+    mid = (turns > 1) & (turns < 4)
+    s = (turns[mid] - 1) / 3
+    assert mid.any() and np.allclose(g[mid], f[mid] * s + f[mid] / 8 * (1 - s), rtol=1e-12, atol=0)
+
+
+def test_rotary_frequencies_refuse(G):
+    for kw in (dict(rotary_dim=0), dict(rotary_dim=7), dict(rotary_dim=-2), dict(base=1.0), dict(base=float("nan")), dict(base=float("inf")),
+               dict(scaling=G.ROTARY_LINEAR, factor=0.5), dict(scaling=G.ROTARY_LINEAR, factor=float("nan")), dict(scaling=G.ROTARY_BASE, rotary_dim=2, factor=2.0),
+               dict(scaling=G.ROTARY_YARN, factor=2.0), dict(scaling=G.ROTARY_YARN, factor=2.0, original_len=100.0, a=1.0, b=2.0),
+               dict(scaling=G.ROTARY_WAVELENGTH, factor=2.0, original_len=100.0, a=4.0, b=1.0)):
+        with pytest.raises(G.OptGqaError) as e:
+            G.rotary_frequencies(**{"rotary_dim": 64, **kw})
+        assert e.value.status == -2, kw
+    for scaling in (5, -1):
+        with pytest.raises(G.OptGqaError) as e:
+            G.rotary_frequencies(64, scaling=scaling)
+        assert e.value.status == -3
+    f = G.load_library().optgqa_rotary_frequencies_host
+    assert f(None, ONE, 64, 10000.0, 0, 1.0, 0.0, 0.0, 0.0) == -1 and f(ONE, None, 64, 10000.0, 0, 1.0, 0.0, 0.0, 0.0) == -1
+
+
+def test_rotary_refuses_before_any_launch(G):
+    lib = G.load_library()
+
+    def rows(q_out=ONE, q=ONE, k_out=ONE, k=ONE, pos=ONE, f=ONE, T=3, Hq=4, Hkv=2, D=64, rot=64, m=1.0, s=(256, 256, 128, 128), dt=0):
+        return lib.optgqa_rotary_embedding(q_out, q, k_out, k, pos, f, T, Hq, Hkv, D, rot, 0, m, 0, *s, dt, None)
+
+    assert rows(T=-1) == -2 and rows(Hq=-1) == -2 and rows(Hq=0, Hkv=0) == -2 and rows(Hq=70000) == -2
+    assert rows(D=96) == -3 and rows(dt=2) == -3
+    assert rows(rot=0) == -2 and rows(rot=66) == -2 and rows(rot=63) == -2
+    assert rows(m=float("nan")) == -2 and rows(m=float("inf")) == -2
+    assert rows(s=(255, 256, 128, 128)) == -2 and rows(s=(256, 255, 128, 128)) == -2 and rows(s=(256, 256, 127, 128)) == -2 and rows(s=(256, 256, 128, 127)) == -2
+    for name in ("q_out", "q", "k_out", "k", "pos", "f"):
+        assert rows(**{name: None}) == -1, name
+    odd = ctypes.c_void_p(17)
+    for name in ("q_out", "q", "k_out", "k", "pos", "f"):
+        assert rows(**{name: odd}) == -3, name
+    assert rows(T=0, q=None, k=None) == 0
+
+    def append(call=lib.optgqa_rotary_and_cache, scales=(), q_out=ONE, q=ONE, k=ONE, v=ONE, kc=ONE, vc=ONE, slots=ONE, pos=ONE, f=ONE, T=3,
+               Hq=4, Hkv=2, D=64, rot=64, m=1.0, bs=16, s=(256, 256, 128, 128), dt=1):
+        return call(q_out, q, k, v, kc, vc, slots, pos, f, T, Hq, Hkv, D, rot, 0, m, bs, *s, *scales, dt, None)
+
+    one, heads = lib.optgqa_rotary_and_cache_fp8, lib.optgqa_rotary_and_cache_fp8_heads
+    for call, scales in ((lib.optgqa_rotary_and_cache, ()), (one, (1.0, 1.0)), (heads, (ONE, ONE))):
+        def a(**kw):
+            return append(call, scales, **kw)
+        assert a(T=-1) == -2 and a(Hq=0) == -2 and a(Hkv=0) == -2 and a(bs=8) == -3 and a(D=32) == -3 and a(dt=9) == -3
+        assert a(rot=65) == -2 and a(m=float("nan")) == -2 and a(s=(256, 256, 128, 100)) == -2 and a(s=(256, 256, 100, 128)) == -2
+        for name in ("q_out", "q", "k", "v", "kc", "vc", "slots", "pos", "f"):
+            assert a(**{name: None}) == -1, name
+        assert a(v=ctypes.c_void_p(17)) == -3
+        assert a(T=0, q=None) == 0
+    assert append(kc=ctypes.c_void_p(17)) == -3
+    for bad in (0.0, -1.0, float("nan"), float("inf")):
+        assert append(one, (bad, 1.0)) == -2 and append(one, (1.0, bad)) == -2
+    assert append(heads, (None, ONE)) == -1 and append(heads, (ONE, None)) == -1
+
+
+def test_the_binding_refuses_what_the_library_cannot_see(G):
+    import torch
+    q, k = torch.zeros(3, 4, 64, dtype=torch.float16), torch.zeros(3, 2, 64, dtype=torch.float16)
+    pos, f = torch.zeros(3, dtype=torch.int32), torch.zeros(32, dtype=torch.float64)
+    with pytest.raises(TypeError):
+        G.rotary_embedding(q, q, k, k, pos.long(), f)
+    with pytest.raises(TypeError):
+        G.rotary_embedding(q, q, k, k, pos, f.float())
+    with pytest.raises(TypeError):
+        G.rotary_embedding(q, q, k, k.bfloat16(), pos, f)
+    with pytest.raises(ValueError):
+        G.rotary_embedding(q, q, k, None, pos, f)
+    with pytest.raises(ValueError):
+        G.rotary_embedding(q, q, k, k, pos, f)                   # not on a GPU
