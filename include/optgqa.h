@@ -48,7 +48,7 @@ extern "C" {
 
 /* Values of every `dtype` argument.  The arguments themselves are plain ints, so that a value
  * outside this list is answered with OPTGQA_ERR_UNSUPPORTED instead of being undefined behaviour. */
-typedef enum { OPTGQA_F16 = 0, OPTGQA_BF16 = 1 } optgqa_dtype;
+typedef enum { OPTGQA_F16 = 0, OPTGQA_BF16 = 1, OPTGQA_F32 = 2 /* optgqa_verify_drafts only */ } optgqa_dtype;
 
 /* partition_size value that asks optgqa_paged_attention for the equal-work split. */
 #define OPTGQA_SPLIT_BALANCED (-2)
@@ -573,6 +573,37 @@ typedef enum {
 int optgqa_rotary_frequencies_host(double *freqs_host, float *magnitude_host, int rotary_dim,
                                    double base, int scaling, double factor, double original_len,
                                    double a, double b);
+
+/*
+ * Verification of drafted tokens (speculative decoding) from given random numbers.  Sequence b has
+ * n_b = cu_draft_lens[b+1] - cu_draft_lens[b] drafts (at most max_drafts are looked at): draft i is token
+ * x = draft_tokens[cu_draft_lens[b] + i], drawn from row cu_draft_lens[b] + i of draft_probs (q); the target model's
+ * distribution at its place (p) is row cu_draft_lens[b] + b + i of target_probs, which has n_b + 1 rows for the sequence.
+ *   - Draft i is kept iff accept_uniforms[cu_draft_lens[b] + i] * q(x) < p(x), the product in 64 bits, up to the first that is not.
+ *     draft_probs == NULL: drafts were certain (q(x) = 1, 0 elsewhere).  An id outside 0 .. vocab_size - 1 is no draft: the
+ *     sequence's drafts end there.
+ *   - The next token is drawn at the first draft that is not kept from r_j = max(p_j - q_j, 0), behind the last kept
+ *     one (or where an id is no draft, or no r_j is positive) from r_j = p_j: the lowest j with
+ *     r_0 + .. + r_j > sample_uniforms[b] * (sum of all r), sums in 64 bits.  Entries that are not finite positive numbers count as 0;
+ *     if all do the token is -1.
+ * tokens[b] = kept drafts, the drawn token, then -1; num_accepted[b] = the number of kept drafts.  Rows need not sum to 1.
+ *
+ *   tokens          [num_seqs][max_drafts + 1] int64
+ *   num_accepted    [num_seqs] int32
+ *   target_probs    [cu_draft_lens[num_seqs] + num_seqs][vocab_size] of dtype (OPTGQA_F32 too), rows target_stride
+ *                   (>= vocab_size) elements apart; draft_probs likewise, one row per draft
+ *   draft_tokens    int64, accept_uniforms fp32 in [0, 1): one per draft (NULL: there are none)
+ *   sample_uniforms [num_seqs] fp32 in [0, 1)
+ *   workspace       optgqa_verify_drafts_workspace_bytes(...) bytes, 16-byte aligned (OPTGQA_ERR_WORKSPACE without it)
+ */
+size_t optgqa_verify_drafts_workspace_bytes(int num_seqs, int vocab_size);
+
+int optgqa_verify_drafts(int64_t *tokens, int32_t *num_accepted, const void *target_probs,
+                         const void *draft_probs, const int64_t *draft_tokens,
+                         const int32_t *cu_draft_lens, const float *accept_uniforms,
+                         const float *sample_uniforms, int num_seqs, int vocab_size, int max_drafts,
+                         int64_t target_stride, int64_t draft_stride, void *workspace,
+                         size_t workspace_bytes, int dtype, void *stream);
 
 /*
  * Diagnostic: un-page the cache (Section III-A: pages are only a re-arrangement of the

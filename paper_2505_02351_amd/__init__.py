@@ -820,5 +820,5 @@ def validate_tables_host(block_tables, context_lens, block_size: int, num_blocks
 from . import operators  # noqa: E402  (uses the helpers above)
 from .operators import (  # noqa: E402, F401
     ROTARY_BASE, ROTARY_LINEAR, ROTARY_PLAIN, ROTARY_WAVELENGTH, ROTARY_YARN, rotary_and_cache, rotary_and_cache_fp8,
-    rotary_and_cache_fp8_heads, rotary_embedding, rotary_frequencies,
+    rotary_and_cache_fp8_heads, rotary_embedding, rotary_frequencies, verify_drafts, verify_drafts_workspace_bytes,
 )

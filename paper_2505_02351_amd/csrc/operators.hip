@@ -1,4 +1,4 @@
-// C ABI of what stands around the attention of a step: rotary positions, rotated cache appends.
+// C ABI of what stands around the attention of a step: rotary positions, rotated cache appends, the verification of drafts.
 // Declarations and the meaning of every argument: include/optgqa.h.
 #include "optgqa.h"
 
@@ -9,6 +9,7 @@
 
 #include "host.hpp"
 #include "rotary_kernels.hpp"
+#include "verify_kernels.hpp"
 
 using namespace optgqa;
 
@@ -142,7 +143,16 @@ int rotary_and_cache_impl(void* q_out, const void* q, const void* k, const void*
     return rotary_impl(c, scales ? RotaryTo::kCacheE4M3 : RotaryTo::kCache, static_cast<hipStream_t>(stream));
 }
 
+template <int DT, int VEC>
+int launch_verify(const VerifyParams& a, int num_seqs, hipStream_t st)
+{
+    const int rc = launch(verify_sums_kernel<DT, VEC>, dim3(num_seqs, a.chunks), dim3(kVerifyThreads), 0, st, a);
+    return rc != OPTGQA_OK ? rc : launch(verify_select_kernel<DT, VEC>, dim3(num_seqs), dim3(kVerifyThreads), 0, st, a);
+}
+
 }  // namespace
+
+static_assert(kF16 == OPTGQA_F16 && kBF16 == OPTGQA_BF16 && kF32 == OPTGQA_F32, "the header's values");
 
 extern "C" {
 
@@ -228,6 +238,55 @@ int optgqa_rotary_and_cache_fp8_heads(void* q_out, const void* q, const void* k,
     const KvScales scales{0.f, 0.f, k_scales, v_scales};
     return rotary_and_cache_impl(q_out, q, k, v, k_cache, v_cache, slot_mapping, positions, freqs, num_tokens, num_heads, num_kv_heads, head_dim,
                                  rotary_dim, interleaved, magnitude, block_size, q_out_stride, q_stride, k_stride, v_stride, &scales, dtype, stream);
+}
+
+size_t optgqa_verify_drafts_workspace_bytes(int num_seqs, int vocab_size)
+{
+    if (num_seqs <= 0 || vocab_size <= 0) return 0;
+    return (size_t)num_seqs * 2 * (((size_t)vocab_size + kVerifyChunk - 1) / kVerifyChunk) * sizeof(double);
+}
+
+int optgqa_verify_drafts(int64_t* tokens, int32_t* num_accepted, const void* target_probs, const void* draft_probs,
+                         const int64_t* draft_tokens, const int32_t* cu_draft_lens, const float* accept_uniforms,
+                         const float* sample_uniforms, int num_seqs, int vocab_size, int max_drafts, int64_t target_stride,
+                         int64_t draft_stride, void* workspace, size_t workspace_bytes, int dtype, void* stream)
+{
+    if (num_seqs < 0 || vocab_size <= 0 || max_drafts < 0 || target_stride < vocab_size || (draft_probs && draft_stride < vocab_size))
+        return OPTGQA_ERR_SHAPE;
+    if (!dtype_ok(dtype) && dtype != OPTGQA_F32) return OPTGQA_ERR_UNSUPPORTED;
+    const int chunks = (int)(((int64_t)vocab_size + kVerifyChunk - 1) / kVerifyChunk);
+    if (chunks > 65535) return OPTGQA_ERR_SHAPE;                 // (2^28 entries)
+    if (num_seqs == 0) return OPTGQA_OK;
+    if (!tokens || !num_accepted || !target_probs || !cu_draft_lens || !sample_uniforms)
+        return OPTGQA_ERR_NULL;
+    const uintptr_t size = dtype == OPTGQA_F32 ? 4 : 2, rows = reinterpret_cast<uintptr_t>(target_probs) | reinterpret_cast<uintptr_t>(draft_probs);
+    if ((rows & (size - 1)) || ((reinterpret_cast<uintptr_t>(tokens) | reinterpret_cast<uintptr_t>(draft_tokens)) & 7u) ||
+        ((reinterpret_cast<uintptr_t>(num_accepted) | reinterpret_cast<uintptr_t>(cu_draft_lens) | reinterpret_cast<uintptr_t>(accept_uniforms) |
+          reinterpret_cast<uintptr_t>(sample_uniforms)) & 3u))
+        return OPTGQA_ERR_UNSUPPORTED;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < optgqa_verify_drafts_workspace_bytes(num_seqs, vocab_size)) return OPTGQA_ERR_WORKSPACE;
+    VerifyParams a;
+    a.tokens = tokens;
+    a.accepted = num_accepted;
+    a.target = target_probs;
+    a.draft = draft_probs;
+    a.draft_tokens = draft_tokens;
+    a.cu = cu_draft_lens;
+    a.accept_u = accept_uniforms;
+    a.sample_u = sample_uniforms;
+    a.sums = static_cast<double*>(workspace);
+    a.target_stride = target_stride;
+    a.draft_stride = draft_stride;
+    a.vocab = vocab_size;
+    a.max_drafts = max_drafts;
+    a.looked_at = draft_tokens && accept_uniforms ? max_drafts : 0;
+    a.chunks = chunks;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    // 16-byte loads where every row lies on 16 bytes
+    const bool wide = !(rows & 15u) && (target_stride | (draft_probs ? draft_stride : 0)) % (int64_t)(16 / size) == 0;
+    if (dtype == OPTGQA_F32) return wide ? launch_verify<kF32, 4>(a, num_seqs, st) : launch_verify<kF32, 1>(a, num_seqs, st);
+    if (dtype == OPTGQA_F16) return wide ? launch_verify<kF16, 8>(a, num_seqs, st) : launch_verify<kF16, 1>(a, num_seqs, st);
+    return wide ? launch_verify<kBF16, 8>(a, num_seqs, st) : launch_verify<kBF16, 1>(a, num_seqs, st);
 }
 
 }  // extern "C"

@@ -1,4 +1,5 @@
-"""Binding of the calls that stand around the attention of a step: rotary positions and rotated cache appends.
+"""Binding of the calls that stand around the attention of a step: rotary positions, rotated cache appends and the
+verification of drafted tokens.
 
 Conventions as in the package: q [T, Hq, D], k and v [T, Hkv, D] with any token stride (dense in their
 last two dims: slices of one projection's rows will do), caches [NB, Hkv, bs, D], positions [T] int32,
@@ -26,9 +27,12 @@ def declare(lib: ctypes.CDLL) -> None:
         "rotary_and_cache": [vp] * 9 + [i32] * 6 + [f32, i32] + [i64] * 4 + [i32, vp],
         "rotary_and_cache_fp8": [vp] * 9 + [i32] * 6 + [f32, i32] + [i64] * 4 + [f32, f32, i32, vp],
         "rotary_and_cache_fp8_heads": [vp] * 9 + [i32] * 6 + [f32, i32] + [i64] * 4 + [vp, vp, i32, vp],
+        "verify_drafts": [vp] * 8 + [i32] * 3 + [i64, i64, vp, ctypes.c_size_t, i32, vp],
     }.items():
         f = getattr(lib, "optgqa_" + name)
         f.restype, f.argtypes = i32, args
+    f = lib.optgqa_verify_drafts_workspace_bytes
+    f.restype, f.argtypes = ctypes.c_size_t, [i32, i32]
 
 
 def rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: int = ROTARY_PLAIN, factor: float = 1.0,
@@ -135,3 +139,53 @@ def rotary_and_cache_fp8_heads(q_out: torch.Tensor, q: torch.Tensor, k: torch.Te
     _pkg._head_scales(q, k_cache, k_scales, v_scales)
     _append("optgqa_rotary_and_cache_fp8_heads", q_out, q, k, v, k_cache, v_cache, slot_mapping, positions, freqs, interleaved, magnitude,
             stream, True, (k_scales.data_ptr(), v_scales.data_ptr()))
+
+
+_PROBABILITIES = {torch.float16: _pkg.F16, torch.bfloat16: _pkg.BF16, torch.float32: 2}
+
+
+def verify_drafts_workspace_bytes(num_seqs: int, vocab_size: int) -> int:
+    """optgqa_verify_drafts_workspace_bytes."""
+    return int(_pkg.load_library().optgqa_verify_drafts_workspace_bytes(num_seqs, vocab_size))
+
+
+def verify_drafts(tokens: torch.Tensor, num_accepted: torch.Tensor, target_probs: torch.Tensor, draft_probs: Optional[torch.Tensor],
+                  draft_tokens: torch.Tensor, cu_draft_lens: torch.Tensor, accept_uniforms: torch.Tensor, sample_uniforms: torch.Tensor,
+                  workspace: Optional[torch.Tensor], stream=None) -> None:
+    """optgqa_verify_drafts: which of the drafts are kept, and each sequence's next token.  tokens [B, max_drafts + 1] int64,
+    target_probs [drafts + B, V] and draft_probs [drafts, V] (or None: drafts were certain) float32, float16 or bfloat16."""
+    lib = _pkg.load_library()
+    if target_probs.dtype not in _PROBABILITIES:
+        raise TypeError(f"optgqa: probabilities must be float32, float16 or bfloat16, got {target_probs.dtype}")
+    if draft_probs is not None and draft_probs.dtype != target_probs.dtype:
+        raise TypeError(f"optgqa: draft_probs must be {target_probs.dtype}, got {draft_probs.dtype}")
+    index = target_probs.get_device()
+    for t, name, want in ((tokens, "tokens", torch.int64), (num_accepted, "num_accepted", torch.int32), (draft_tokens, "draft_tokens", torch.int64),
+                          (cu_draft_lens, "cu_draft_lens", torch.int32), (accept_uniforms, "accept_uniforms", torch.float32),
+                          (sample_uniforms, "sample_uniforms", torch.float32)):
+        if t.dtype != want:
+            raise TypeError(f"optgqa: {name} must be {want}, got {t.dtype}")
+        if not t.is_cuda or t.get_device() != index or not t.is_contiguous():
+            raise ValueError(f"optgqa: {name} must be a dense tensor on the probabilities' GPU")
+    if draft_probs is not None and draft_probs.get_device() != index:
+        raise ValueError("optgqa: draft_probs must be on the same GPU as target_probs")
+    B, T = num_accepted.shape[0], draft_tokens.shape[0]
+    if target_probs.dim() != 2 or tokens.dim() != 2:
+        raise ValueError("optgqa: tokens and target_probs must have two dimensions")
+    V = target_probs.shape[1]
+    if (tokens.shape[0] != B or tokens.shape[1] < 1 or target_probs.shape[0] != T + B or cu_draft_lens.shape != (B + 1,)
+            or accept_uniforms.shape != (T,) or sample_uniforms.shape != (B,) or (draft_probs is not None and draft_probs.shape != (T, V))):
+        raise ValueError("optgqa: shape mismatch between the tokens, probabilities, drafts and random numbers")
+    for t, name in ((target_probs, "target_probs"), (draft_probs, "draft_probs")):
+        if t is not None and t.shape[0] and t.stride(1) != 1 and V > 1:
+            raise ValueError(f"optgqa: {name} must have dense rows")
+    ws_bytes = _pkg._workspace(workspace, target_probs)
+    rc = lib.optgqa_verify_drafts(tokens.data_ptr(), num_accepted.data_ptr(), target_probs.data_ptr(), _pkg._ptr(draft_probs),
+                                  draft_tokens.data_ptr(), cu_draft_lens.data_ptr(), accept_uniforms.data_ptr(), sample_uniforms.data_ptr(),
+                                  B, V, tokens.shape[1] - 1, _row_stride(target_probs), 0 if draft_probs is None else _row_stride(draft_probs),
+                                  _pkg._ptr(workspace), ws_bytes, _PROBABILITIES[target_probs.dtype], _pkg._stream(stream))
+    _pkg._check(rc, "optgqa_verify_drafts")
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]

@@ -33,3 +33,36 @@ def half_step(ref, eps, smallest):
 
 EPS = {"f16": 2.0 ** -10, "bf16": 2.0 ** -7, "e4m3": 2.0 ** -3}
 SMALLEST = {"f16": 2.0 ** -24, "bf16": 2.0 ** -133, "e4m3": 2.0 ** -9}
+
+
+def verify(target, draft, draft_tokens, cu, accept_u, sample_u, width):
+    """(tokens [B, width], accepted [B]); target, draft float64 rows (draft may be None)."""
+    V, B = target.shape[1], len(cu) - 1
+    tokens, accepted = np.full((B, width), -1, np.int64), np.zeros(B, np.int32)
+
+    def counted(x):
+        return np.where(np.isfinite(x) & (x > 0), x, 0.0)
+
+    for b in range(B):
+        n, count, row = 0, min(cu[b + 1] - cu[b], width - 1), cu[b] + b
+        while n < count:
+            i, x = cu[b] + n, draft_tokens[cu[b] + n]
+            if not (0 <= x < V and accept_u[i] * (1.0 if draft is None else draft[i, x]) < target[row + n, x]):
+                break
+            tokens[b, n] = x
+            n += 1
+        rest = counted(target[row + n])
+        if n < count and 0 <= draft_tokens[cu[b] + n] < V:
+            i, x = cu[b] + n, draft_tokens[cu[b] + n]
+            if draft is None:
+                less = rest.copy()
+                less[x] = 0.0
+            else:
+                with np.errstate(invalid="ignore"):
+                    less = counted(target[row + n] - draft[i])
+            rest = less if less.sum() > 0 else rest
+        sums = np.cumsum(rest)
+        over = (rest > 0) & (sums > sample_u[b] * sums[-1])
+        tokens[b, n] = np.argmax(over) if over.any() else -1
+        accepted[b] = n
+    return tokens, accepted

@@ -108,3 +108,21 @@ def test_the_binding_refuses_what_the_library_cannot_see(G):
         G.rotary_embedding(q, q, k, None, pos, f)
     with pytest.raises(ValueError):
         G.rotary_embedding(q, q, k, k, pos, f)                   # not on a GPU
+
+
+def test_verification_refuses_before_any_launch(G):
+    lib = G.load_library()
+    need = G.verify_drafts_workspace_bytes(3, 32000)
+    assert need == 3 * 2 * 8 * 8 and G.verify_drafts_workspace_bytes(0, 5) == 0 and G.verify_drafts_workspace_bytes(5, 0) == 0
+
+    def v(tokens=ONE, n=ONE, p=ONE, q=ONE, ids=ONE, cu=ONE, a=ONE, s=ONE, B=3, V=32000, most=4, ps=32000, qs=32000, ws=ONE, wsb=None, dt=2):
+        return lib.optgqa_verify_drafts(tokens, n, p, q, ids, cu, a, s, B, V, most, ps, qs, ws, need if wsb is None else wsb, dt, None)
+
+    assert v(B=-1) == -2 and v(V=0) == -2 and v(most=-1) == -2 and v(ps=31999) == -2 and v(qs=31999) == -2 and v(V=2**30, ps=2**30, qs=2**30) == -2
+    assert v(dt=3) == -3 and v(dt=-1) == -3
+    for name in ("tokens", "n", "p", "cu", "s"):
+        assert v(**{name: None}) == -1, name
+    for name, at in (("tokens", 20), ("n", 18), ("p", 18), ("q", 18), ("ids", 20), ("cu", 18), ("a", 18), ("s", 18)):
+        assert v(**{name: ctypes.c_void_p(at)}) == -3, name
+    assert v(ws=None) == -4 and v(wsb=need - 1) == -4 and v(ws=ctypes.c_void_p(8)) == -4
+    assert v(B=0, tokens=None) == 0
