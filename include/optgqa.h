@@ -575,6 +575,63 @@ int optgqa_rotary_frequencies_host(double *freqs_host, float *magnitude_host, in
                                    double a, double b);
 
 /*
+ * Attention for a batch with one common prefix, which is computed once for the whole batch.  The positions
+ * 0 .. num_prefix_blocks * block_size - 1 of every sequence lie in the blocks prefix_table[0 ..]; what lies behind is in each
+ * sequence's own block_tables row, as for the other calls (entry j / block_size for position j; entries below
+ * num_prefix_blocks are not read).  Sequence b has n_b = cu_q_lens[b+1] - cu_q_lens[b] new query tokens, all
+ * already cached, at positions context_lens[b] - n_b .. context_lens[b] - 1; each sees the keys up to its own position:
+ *     s_j = scale * <q, K_g[j]> + alibi_slopes[h] * (j - pos), j = 0 .. pos;   out = sum_j softmax(s)_j V_g[j]
+ * - what optgqa_paged_attention (n_b = 1) and optgqa_paged_prefill give on full tables, to rounding - for decode steps, for
+ * drafted tokens that are verified together (n_b = drafts + 1), and for chunks.  The prefix's keys are read once for 128 rows
+ * (new tokens x heads of a group) of any sequences, as matrix products.  A context may be shorter than the prefix;
+ * a row that sees no key (a negative position, or a token behind cu_q_lens[num_seqs]) is +0.
+ *
+ *   out, q          [num_tokens][num_heads][head_dim]; num_tokens >= cu_q_lens[num_seqs]
+ *   prefix_table    [num_prefix_blocks] int32, full blocks; num_prefix_blocks may be 0
+ *   cu_q_lens       [num_seqs + 1] int32 prefix sums, or NULL: one new token each (num_tokens == num_seqs)
+ *   max_context_len, max_q_len   upper bounds on the context lengths (prefix included) and the n_b; they size the launch
+ *   workspace       optgqa_common_prefix_workspace_bytes(...) bytes, 16-byte aligned (OPTGQA_ERR_WORKSPACE without it)
+ * The 8-bit calls run over E4M3 caches, scales as for optgqa_paged_attention_fp8 and _fp8_heads.  Other arguments and errors as
+ * optgqa_paged_attention.  Infinities and NaN in
+ * keys and values that a row does not see do not reach it; an infinite value that it sees makes that element of it no
+ * finite number (with bf16 it may be NaN).
+ */
+size_t optgqa_common_prefix_workspace_bytes(int num_tokens, int num_seqs, int num_heads,
+                                            int num_kv_heads, int head_dim, int block_size,
+                                            int num_prefix_blocks, int max_context_len,
+                                            int max_q_len);
+
+int optgqa_paged_attention_common(void *out, const void *q, const void *k_cache, const void
+                                  *v_cache, const int32_t *prefix_table, const int32_t
+                                  *block_tables, const int32_t *context_lens, const int32_t
+                                  *cu_q_lens, const float *alibi_slopes, float scale, int
+                                  num_tokens, int num_seqs, int num_heads, int num_kv_heads, int
+                                  head_dim, int block_size, int num_prefix_blocks, int
+                                  max_blocks_per_seq, int max_context_len, int max_q_len, void
+                                  *workspace, size_t workspace_bytes, int dtype, void *stream);
+
+int optgqa_paged_attention_common_fp8(void *out, const void *q, const void *k_cache, const void
+                                      *v_cache, const int32_t *prefix_table, const int32_t
+                                      *block_tables, const int32_t *context_lens, const int32_t
+                                      *cu_q_lens, const float *alibi_slopes, float scale, float
+                                      k_scale, float v_scale, int num_tokens, int num_seqs, int
+                                      num_heads, int num_kv_heads, int head_dim, int block_size, int
+                                      num_prefix_blocks, int max_blocks_per_seq, int
+                                      max_context_len, int max_q_len, void *workspace, size_t
+                                      workspace_bytes, int dtype, void *stream);
+
+int optgqa_paged_attention_common_fp8_heads(void *out, const void *q, const void *k_cache, const
+                                            void *v_cache, const int32_t *prefix_table, const
+                                            int32_t *block_tables, const int32_t *context_lens,
+                                            const int32_t *cu_q_lens, const float *alibi_slopes,
+                                            float scale, const float *k_scales, const float
+                                            *v_scales, int num_tokens, int num_seqs, int num_heads,
+                                            int num_kv_heads, int head_dim, int block_size, int
+                                            num_prefix_blocks, int max_blocks_per_seq, int
+                                            max_context_len, int max_q_len, void *workspace, size_t
+                                            workspace_bytes, int dtype, void *stream);
+
+/*
  * Verification of drafted tokens (speculative decoding) from given random numbers.  Sequence b has
  * n_b = cu_draft_lens[b+1] - cu_draft_lens[b] drafts (at most max_drafts are looked at): draft i is token
  * x = draft_tokens[cu_draft_lens[b] + i], drawn from row cu_draft_lens[b] + i of draft_probs (q); the target model's

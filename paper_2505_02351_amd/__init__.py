@@ -819,6 +819,7 @@ def validate_tables_host(block_tables, context_lens, block_size: int, num_blocks
 
 from . import operators  # noqa: E402  (uses the helpers above)
 from .operators import (  # noqa: E402, F401
-    ROTARY_BASE, ROTARY_LINEAR, ROTARY_PLAIN, ROTARY_WAVELENGTH, ROTARY_YARN, rotary_and_cache, rotary_and_cache_fp8,
-    rotary_and_cache_fp8_heads, rotary_embedding, rotary_frequencies, verify_drafts, verify_drafts_workspace_bytes,
+    ROTARY_BASE, ROTARY_LINEAR, ROTARY_PLAIN, ROTARY_WAVELENGTH, ROTARY_YARN, common_prefix_workspace_bytes, paged_attention_common,
+    paged_attention_common_fp8, paged_attention_common_fp8_heads, rotary_and_cache, rotary_and_cache_fp8, rotary_and_cache_fp8_heads,
+    rotary_embedding, rotary_frequencies, verify_drafts, verify_drafts_workspace_bytes,
 )

@@ -150,6 +150,11 @@ __device__ __forceinline__ int wave_max(int x)
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Softmax references that are moved lazily (decode_mc_kernels.hpp):
+constexpr float kRescaleThreshold = 30.f;    // log2 units: rescale when a tile maximum exceeds the reference by this
+constexpr float kRescaleHeadroom = 60.f;     // ... and then put the reference this far ABOVE the maximum
+constexpr float kNoMax = -1.0e30f;           // "no key seen yet"; finite so that differences stay finite
+
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 // eight E4M3 codes (two dwords) -> eight DT values (one MFMA operand), exactly: every E4M3 value is

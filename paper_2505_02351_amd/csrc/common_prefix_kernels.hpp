@@ -1,0 +1,610 @@
+// Attention for a batch whose sequences all begin with the same cached blocks: the common prefix is computed once for all.
+//
+// Softmax over a row's keys can be cut anywhere: a piece leaves its reference m, its sum l = sum 2^(s - m) and its weighted
+// sum o = sum 2^(s - m) V, and pieces join as
+//     out = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i,   M = max m_i          (s: scores in base 2)
+// Here the cuts are
+//   the prefix     the rows of ALL sequences - every new token, every head of the group - against its keys, cut into ranges of
+//                  p_keys: a dense contraction whose K and V tiles serve up to 128 rows at a time;
+//   own parts      the rows of ONE sequence against the keys behind the prefix, cut into ranges of s_keys.
+// One launch computes all pieces (a workgroup each), a second joins them.  A row sees keys 0 .. its position, wherever the
+// prefix ends.
+//
+// A workgroup is four waves of 32 rows: RW row blocks by KS key groups, RW * KS = 4.  The waves of a key group share its
+// tiles of 32 keys in LDS; the KS groups take tiles in turn, and their results are joined through LDS.  With many rows 4 x 1 reads
+// each tile once for 128 rows, with few (a sequence's own part: the heads of a group, times its new tokens) 1 x 4 lets each wave
+// stream tiles of its own.  Scores, softmax and output as in prefill_kernels.hpp: both contractions transposed on
+// v_mfma_f32_32x32x16, sums and output in fp32, weights rounded to fp16 once or split into two bf16.
+#pragma once
+#include <type_traits>
+
+#include "mfma_tiles.hpp"
+
+namespace optgqa {
+
+constexpr int kCommonThreads = 256, kCommonWaves = 4;
+constexpr int kCommonBuffers = 4;               // tile buffers (a K and a V tile) of a workgroup, over its key groups
+
+struct CommonParams {
+    void* out;                  // [T][Hq][D]
+    const void* q;
+    const void* k_cache;        // [NB][Hkv][bs][D]
+    const void* v_cache;
+    const int32_t* prefix_table;
+    const int32_t* block_tables;
+    const int32_t* context_lens;
+    const int32_t* cu_q_lens;   // [B + 1], or nullptr: a new token each
+    const float* slopes;        // [Hq] or nullptr
+    float scale2, out_scale;    // log2(e) * scale (times k_scale); v_scale
+    const float *k_scales, *v_scales;           // E4M3 caches, one pair per KV head, or nullptr
+    int num_tokens, num_seqs, num_heads, num_kv_heads, group, block_shift, max_blocks_per_seq;
+    int prefix_len;             // keys
+    int rows;                   // num_tokens * group: of a KV head
+    int p_row_waves, p_tiles, p_splits, p_keys, p_units, p_workgroups;      // tiles: workgroups' row tiles; units: KV head, range
+    int s_row_waves, s_tiles, s_splits, s_keys, s_units;                    // units: sequence, KV head, range
+    // pieces, 32 rows each: of the prefix [range][KV head][p_slots], then own ones [range][KV head][s_slots]
+    int p_slots, s_slots;
+    int64_t s_first;
+    float4* o;                  // per piece [D / 8][64]: what lane l of the wave holds, dims 8i + 4 (l / 32) .. + 3 of row l % 32
+    float2* ml;                 // per piece [32]: m, l
+    FastDiv by_group, by_p_tiles, by_s_tiles, by_kv_heads, by_seqs;
+};
+
+template <int D> constexpr int kCommonLds = [] {
+    const int tiles = kCommonBuffers * 2 * PfDirect<D>::kTile, join = kCommonWaves * 64 * (D / 8 * 16 + 8);
+    return tiles > join ? tiles : join;
+}();
+
+// The sequence of token t and the token's position in it; seq < 0: no sequence has it.  All lanes of a wave together, a
+// sequence's end a lane, 64 at a time.
+struct TokenPlace { int seq, pos; };
+__device__ __forceinline__ TokenPlace place_of_token(const CommonParams& p, int t)
+{
+    if (!p.cu_q_lens) return {t, p.context_lens[t] - 1};
+    const int lane = threadIdx.x & 63;
+    int b = 0;
+    for (int first = 0; first < p.num_seqs; first += 64) {
+        const int n = min(p.num_seqs - first, 64);
+        const int end = p.cu_q_lens[first + min(lane, n - 1) + 1];
+        int k = 0;                                               // of the n sequences, those that end at or before t
+#pragma unroll
+        for (int s = 32; s; s >>= 1)
+            if (k + s <= n && __shfl(end, k + s - 1) <= t) k += s;
+        if (k + 1 <= n && __shfl(end, k) <= t) ++k;
+        b += k;
+    }
+    if (b >= p.num_seqs) return {-1, -1};
+    return {b, p.context_lens[b] - p.cu_q_lens[b + 1] + t};
+}
+
+// A workgroup's rows and keys.
+struct CommonJob {
+    bool prefix;
+    int g;
+    const int32_t* table;
+    int kbeg, kend;             // keys; kend > kbeg
+    int row0, num_rows;         // its first row, of the batch's (prefix) or of the sequence's
+    int tok0, pos0;             // token and position of row 0 (pos0: own parts)
+    int64_t slot;               // piece of its first 32 rows
+};
+
+template <int DT> __device__ __forceinline__ bool any_not_finite(uint4 x)
+{
+    constexpr uint32_t kExp = DT == kF16 ? 0x7c00u : 0x7f80u;
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w = i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w;
+        odd = odd || (w & kExp) == kExp || ((w >> 16) & kExp) == kExp;
+    }
+    return odd;
+}
+
+// a pair of 2-byte values with those that are no finite numbers put to 0
+template <int DT> __device__ __forceinline__ uint32_t finite_pair(uint32_t w)
+{
+    constexpr uint32_t kExp = DT == kF16 ? 0x7c00u : 0x7f80u;
+    if ((w & kExp) == kExp) w &= 0xffff0000u;
+    if (((w >> 16) & kExp) == kExp) w &= 0x0000ffffu;
+    return w;
+}
+
+template <int DT, bool KV8, int D, int RW>
+__device__ __forceinline__ void common_body(const CommonParams& p, const CommonJob& job)
+{
+    constexpr int KS = kCommonWaves / RW, NBUF = kCommonBuffers / KS;
+    constexpr int kQ = D / 16, kDB = D / 32, kPieces = D / 8;
+    constexpr int ES = KV8 ? 1 : 2;
+    typedef PfDirect<D> Tile;
+    constexpr int kWaveGroups = Tile::kGroups / RW;              // 1 KiB groups of a K (or V) tile that a wave brings
+    constexpr int kHalves = RW == 1 ? 2 : 1;                     // runs of up to 16 keys, each in one block, they lie in
+    constexpr int kRunGroups = kWaveGroups / kHalves;
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    extern __shared__ __attribute__((aligned(16))) unsigned char common_lds[];
+    unsigned char* const lds = common_lds;
+    const int lane = threadIdx.x & 63, n32 = lane & 31, h2 = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rw = wave % RW, kw = wave / RW;
+    const int kbeg = job.kbeg, kend = job.kend;
+    const int ntiles = (kend - kbeg + kPfKeys - 1) / kPfKeys, steps = (ntiles + KS - 1) / KS;
+    auto has = [&](int j) __attribute__((always_inline)) { return j * KS + kw < ntiles; };
+
+    // ---- where tiles come from: a lane holds one of 64 block numbers -------------------------------------
+    const int bshift = p.block_shift, bmask = (1 << bshift) - 1;
+    const uint32_t blk_bytes = (uint32_t)p.num_kv_heads << bshift << (D == 128 ? 7 : 6) << (ES - 1);
+    const uint32_t head_bytes = (uint32_t)job.g << bshift << (D == 128 ? 7 : 6) << (ES - 1);
+    const unsigned char* const kc = static_cast<const unsigned char*>(p.k_cache) + head_bytes;
+    const unsigned char* const vc = static_cast<const unsigned char*>(p.v_cache) + head_bytes;
+    const int last_block = (kend - 1) >> bshift;
+    int held_first = kbeg >> bshift;
+    int held = job.table[min(held_first + lane, last_block)];
+    const int load_row = Tile::load_row(lane), load_col = Tile::load_col(lane);
+    const uint32_t lane_off = (uint32_t)(load_row * D * ES + 8 * load_col * ES);
+    // byte offset, in either cache from its KV head's first block on, of key `key` (wave-uniform)
+    auto key_at = [&](int key) __attribute__((always_inline)) -> uint64_t {
+        const int block = key >> bshift;
+        if (__builtin_expect(block - held_first >= 64, 0)) {
+            held_first = block;
+            held = job.table[min(held_first + lane, last_block)];
+        }
+        return (uint64_t)(uint32_t)__builtin_amdgcn_readlane(held, block - held_first) * blk_bytes + (uint32_t)((key & bmask) * (D * ES));
+    };
+    // offsets, and this lane's, of the wave's runs of the group's tile j
+    struct Runs { uint64_t at[kHalves]; uint32_t lane_at[kWaveGroups]; };
+    auto runs_of = [&](int j) __attribute__((always_inline)) {
+        Runs r;
+        const int key0 = kbeg + kPfKeys * (j * KS + kw) + rw * (kPfKeys / RW);
+        const bool tail = key0 + kPfKeys / RW > kend;            // keys from kend on: kend - 1 again
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) r.at[h] = key_at(min(key0 + 16 * h, kend - 1));
+#pragma unroll
+        for (int n = 0; n < kWaveGroups; ++n) {
+            r.lane_at[n] = (uint32_t)((n % kRunGroups) * Tile::kRows * D * ES) + lane_off;
+            if (tail) {
+                const int first = min(key0 + 16 * (n / kRunGroups), kend - 1);
+                const int key = min(key0 + n * Tile::kRows + load_row, kend - 1);
+                r.lane_at[n] = (uint32_t)((key - first) * (D * ES) + 8 * load_col * ES);
+            }
+        }
+        return r;
+    };
+    auto buffer = [&](int j) __attribute__((always_inline)) { return (kw * NBUF + (j & (NBUF - 1))) * 2 * Tile::kTile; };     // K tile, then V tile
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
+    // 2-byte caches: straight to LDS
+    auto ask = [&](const Runs& r, const unsigned char* cache, int at) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < kWaveGroups; ++n)
+            load_direct(lds0 + at + (rw * kWaveGroups + n) * Tile::kGroup, cache + r.at[n / kRunGroups], r.lane_at[n]);
+    };
+    // 8-bit caches: codes to registers, widened on the way into LDS
+    u32x2 stage_k[KV8 ? kWaveGroups : 1], stage_v[KV8 ? kWaveGroups : 1];
+    auto fetch = [&](const Runs& r, const unsigned char* cache, u32x2* stage) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < kWaveGroups; ++n)
+            stage[n] = *reinterpret_cast<const u32x2*>(cache + r.at[n / kRunGroups] + r.lane_at[n]);
+    };
+    auto put = [&](const u32x2* stage, int at) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < kWaveGroups; ++n)
+            *reinterpret_cast<uint4*>(lds + at + (rw * kWaveGroups + n) * Tile::kGroup + 16 * lane) = widen8_e4m3<DT>(stage[n][0], stage[n][1]);
+    };
+
+    // ---- the lane's row ---------------------------------------------------------------------------------
+    const int r = job.row0 + 32 * rw + n32;
+    const bool row_ok = r < job.num_rows;
+    const int rc = min(r, job.num_rows - 1), ti = p.by_group.div(rc), head = job.g * p.group + (rc - ti * p.group);
+    const int t = job.tok0 + ti;
+    const int pos = job.prefix ? place_of_token(p, t).pos : job.pos0 + ti;
+    const int lim = row_ok ? min(pos + 1, kend) : kend;          // keys below it are visible
+    const int least = -wave_max(-lim);                           // tiles that end at or below it need no mask
+    uint4 qb[kQ];
+    {
+        const unsigned char* const qp = static_cast<const unsigned char*>(p.q) + ((int64_t)t * p.num_heads + head) * (D * 2) + 16 * h2;
+#pragma unroll
+        for (int m = 0; m < kQ; ++m) {
+            qb[m] = *reinterpret_cast<const uint4*>(qp + 32 * m);
+            if (!row_ok) qb[m] = make_uint4(0u, 0u, 0u, 0u);
+        }
+    }
+    const float scale2 = KV8 && p.k_scales ? p.scale2 * p.k_scales[job.g] : p.scale2;
+    const float slope2 = row_ok && p.slopes ? p.slopes[head] * kLog2e : 0.f;
+    const float posf = (float)pos;
+    f32x16 key_bias;                                             // slope * (key's offset in its tile) / score scale: the scores start from it
+    {
+        const float per_key = slope2 / scale2;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) key_bias[e] = per_key * (float)(8 * (e >> 2) + (e & 3));
+    }
+    f32x16 acc[kDB];
+#pragma unroll
+    for (int db = 0; db < kDB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[db][e] = 0.f;
+    float m_ref = 0.f, lsum = 0.f;
+    bool started = !row_ok;
+
+    const int k_at = Tile::row_at(n32, h2);
+    auto scores = [&](int at) __attribute__((always_inline)) {
+        f32x16 st = key_bias;
+#pragma unroll
+        for (int m = 0; m < kQ; ++m)
+            st = mfma32<DT>(*reinterpret_cast<const uint4*>(lds + at + k_at + Tile::dims_at(m)), qb[m], st);
+        return st;
+    };
+    uint32_t pk[2][4], pk_lo[2][4];                              // weights as pairs of 2-byte values (and what is left of them)
+    // key0: the tile's first key
+    auto softmax = [&](int key0, f32x16 st, auto masked) __attribute__((always_inline)) {
+        constexpr bool MASKED = decltype(masked)::value;
+        const float b0 = fmaf(slope2, (float)(key0 + 4 * h2) - posf, -m_ref);
+        float x[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            x[e] = fmaf(st[e], scale2, b0);
+            if (MASKED) x[e] = key0 + 4 * h2 + 8 * (e >> 2) + (e & 3) < lim ? x[e] : -INFINITY;
+        }
+        float mx = x[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) mx = fmaxf(mx, x[e]);
+        const bool first = !started;
+        if (__builtin_amdgcn_ballot_w64(first || mx > PfSoftmax<DT>::kThreshold) != 0) {
+            mx = fmaxf(mx, __shfl_xor(mx, 32));                  // the row's keys live in 2 lanes (h2)
+            const bool sees = mx > -INFINITY;
+            const float delta = first ? (sees ? mx + PfSoftmax<DT>::kHeadroom : 0.f) : fmaxf(mx + PfSoftmax<DT>::kHeadroom, 0.f);
+            const float alpha = first ? 1.f : fast_exp2(-delta);
+            started = started || sees;
+            m_ref += delta;
+            lsum *= alpha;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] -= delta;
+#pragma unroll
+            for (int db = 0; db < kDB; ++db)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[db][e] *= alpha;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float w0 = fast_exp2(x[2 * e]), w1 = fast_exp2(x[2 * e + 1]);
+            if (PfSoftmax<DT>::kSplitWeights) {
+                split_bf16(w0, w1, pk[e >> 2][e & 3], pk_lo[e >> 2][e & 3]);
+                lsum += w0 + w1;
+            } else {
+                // one rounding: the sum is that of the weights as rounded, the output an exact convex combination
+                const uint32_t two = narrow2<DT>(w0, w1);
+                pk[e >> 2][e & 3] = two;
+                lsum += widen_lo<DT>(two) + widen_hi<DT>(two);
+            }
+        }
+    };
+    typedef short i16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) i16x4* lds_i16x4_ptr;
+    const int v_at = Tile::keys_at(lane & 15, (lane >> 4) & 1, h2);
+    // keys 16m + 4 h2 .. + 3 and 16m + 8 + 4 h2 .. + 3 of dim 32 db + n32
+    auto v_operand = [&](int at, int m, int db) __attribute__((always_inline)) {
+        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_ptr)(lds + at + v_at + Tile::further(2 * m, db)));
+        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_ptr)(lds + at + v_at + Tile::further(2 * m + 1, db)));
+        const uint2 lo2 = __builtin_bit_cast(uint2, lo), hi2 = __builtin_bit_cast(uint2, hi);
+        return make_uint4(lo2.x, lo2.y, hi2.x, hi2.y);
+    };
+    auto weighted = [&](uint4 va, int m, f32x16 c) __attribute__((always_inline)) {
+        c = mfma32<DT>(va, make_uint4(pk[m][0], pk[m][1], pk[m][2], pk[m][3]), c);
+        if (PfSoftmax<DT>::kSplitWeights) c = mfma32<DT>(va, make_uint4(pk_lo[m][0], pk_lo[m][1], pk_lo[m][2], pk_lo[m][3]), c);
+        return c;
+    };
+    auto output = [&](int at) __attribute__((always_inline)) {
+#pragma unroll
+        for (int db = 0; db < kDB; ++db)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) acc[db] = weighted(v_operand(at, m, db), m, acc[db]);
+    };
+    // A tile that some row's end cuts.  A weight of 0 does not hide a V that is no finite number from the matrix instruction.  Where
+    // such a V lies beyond some row's end, the matrix instructions see 0 in its place, and the rows that do see its
+    // key get it by itself (a positive weight times it is it again).
+    auto output_cut = [&](int key0, int at) __attribute__((always_inline)) {
+        bool odd = false;
+#pragma unroll
+        for (int n = 0; n < Tile::kGroups; ++n)
+            odd = odd || (key0 + n * Tile::kRows + load_row >= least && any_not_finite<DT>(*reinterpret_cast<const uint4*>(lds + at + n * Tile::kGroup + 16 * lane)));
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) == 0, 1)) {
+            output(at);
+            return;
+        }
+#pragma unroll
+        for (int db = 0; db < kDB; ++db)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                const uint4 va = v_operand(at, m, db);
+                acc[db] = weighted(make_uint4(finite_pair<DT>(va.x), finite_pair<DT>(va.y), finite_pair<DT>(va.z), finite_pair<DT>(va.w)), m, acc[db]);
+            }
+#pragma unroll 1
+        for (int k = 0; k < kPfKeys; ++k) {
+            const bool sees = key0 + k < lim;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {                  // dims 8i + 4 h2 .. + 3
+                const uint2 v = *reinterpret_cast<const uint2*>(lds + at + Tile::row_at(k, i & 1) + Tile::dims_at(i >> 1) + 8 * h2);
+                const uint32_t bad[2] = {v.x ^ finite_pair<DT>(v.x), v.y ^ finite_pair<DT>(v.y)};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float x = j & 1 ? widen_hi<DT>(bad[j >> 1]) : widen_lo<DT>(bad[j >> 1]);
+                    acc[i >> 2][4 * (i & 3) + j] += sees ? x : 0.f;
+                }
+            }
+        }
+    };
+    auto first_key = [&](int j) __attribute__((always_inline)) { return kbeg + kPfKeys * (j * KS + kw); };
+    auto weigh = [&](int j, f32x16 st) __attribute__((always_inline)) {
+        const int key0 = first_key(j);
+        if (key0 + kPfKeys > least) softmax(key0, st, std::true_type{});
+        else softmax(key0, st, std::false_type{});
+    };
+    auto add = [&](int j, int at) __attribute__((always_inline)) {
+        const int key0 = first_key(j);
+        if (key0 + kPfKeys > least) output_cut(key0, at);
+        else output(at);
+    };
+    auto reads_done = [] __attribute__((always_inline)) () { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
+
+    // ---- the walk -----------------------------------------------------------------------------------------
+    if constexpr (RW > 1) {
+        // a key group's tiles in a ring of NBUF buffers, asked for NBUF - 1 steps ahead; one barrier a step
+        constexpr int kLoads = 2 * kWaveGroups;                  // of a wave, per tile
+        auto bring = [&](int j) __attribute__((always_inline)) {
+            const Runs runs = runs_of(j);
+            if constexpr (KV8) {
+                fetch(runs, kc, stage_k);
+                fetch(runs, vc, stage_v);
+            } else {
+                ask(runs, kc, buffer(j));
+                ask(runs, vc, buffer(j) + Tile::kTile);
+            }
+        };
+        auto land = [&](int j) __attribute__((always_inline)) {  // 8-bit caches: what was fetched last
+            put(stage_k, buffer(j));
+            put(stage_v, buffer(j) + Tile::kTile);
+        };
+        if constexpr (KV8) {
+            if (has(0)) {
+                bring(0);
+                land(0);
+            }
+            if (has(1)) bring(1);
+        } else {
+#pragma unroll
+            for (int j = 0; j < NBUF - 1; ++j)
+                if (has(j)) bring(j);
+        }
+        for (int j = 0; j < steps; ++j) {
+            if constexpr (!KV8) {
+                if (NBUF > 2 && has(j + NBUF - 2)) wait_direct<(NBUF - 2) * kLoads>();
+                else wait_direct();
+            }
+            __syncthreads();                                     // tile j is there for all, the buffer of tile j - 1 free
+            if constexpr (KV8) {
+                if (has(j + 1)) land(j + 1);
+                if (has(j + 2)) bring(j + 2);
+            } else {
+                if (has(j + NBUF - 1)) bring(j + NBUF - 1);
+            }
+            if (has(j)) {
+                weigh(j, scores(buffer(j)));
+                add(j, buffer(j) + Tile::kTile);
+            }
+        }
+    } else {
+        // a wave's own tiles, one buffer: the next K tile is asked for when this one's scores are there, the next V
+        // tile when this one's output is
+        const int at_k = buffer(0), at_v = at_k + Tile::kTile;
+        Runs runs;
+        if (has(0)) {
+            runs = runs_of(0);
+            if constexpr (KV8) {
+                fetch(runs, kc, stage_k);
+                fetch(runs, vc, stage_v);
+            } else {
+                ask(runs, kc, at_k);
+                ask(runs, vc, at_v);
+            }
+        }
+        for (int j = 0; has(j); ++j) {
+            const bool more = has(j + 1);
+            if constexpr (KV8) {
+                put(stage_k, at_k);
+                put(stage_v, at_v);
+                if (more) {
+                    runs = runs_of(j + 1);
+                    fetch(runs, kc, stage_k);
+                    fetch(runs, vc, stage_v);
+                }
+                wave_lds_fence();
+                weigh(j, scores(at_k));
+                add(j, at_v);
+                wave_lds_fence();
+            } else {
+                wait_direct<kWaveGroups>();                      // (V tile j is newer)
+                const f32x16 st = scores(at_k);
+                reads_done();
+                if (more) {
+                    runs = runs_of(j + 1);
+                    ask(runs, kc, at_k);
+                }
+                weigh(j, st);
+                if (more) wait_direct<kWaveGroups>();
+                else wait_direct();
+                add(j, at_v);
+                reads_done();
+                if (more) ask(runs, vc, at_v);
+            }
+        }
+    }
+
+    // ---- what it leaves: the key groups' results joined, one piece for each row block ---------------------------
+    const float l_row = lsum + __shfl_xor(lsum, 32);
+    const float m_row = started && row_ok ? m_ref : -INFINITY;
+    const bool exists = job.row0 + 32 * rw < job.num_rows;       // wave-uniform
+    float4* const o = p.o + (job.slot + rw) * (kPieces * 64) + lane;
+    float2* const ml = p.ml + (job.slot + rw) * 32 + n32;
+    auto piece_of = [&](int i) __attribute__((always_inline)) {
+        const f32x16& a = acc[i >> 2];
+        const int e = 4 * (i & 3);
+        return make_float4(a[e], a[e + 1], a[e + 2], a[e + 3]);
+    };
+    if constexpr (KS == 1) {
+        if (!exists) return;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) o[64 * i] = piece_of(i);
+        if (h2 == 0) *ml = make_float2(m_row, l_row);
+    } else {
+        float4* const xo = reinterpret_cast<float4*>(lds);       // [wave][piece][lane]
+        float2* const xml = reinterpret_cast<float2*>(lds + kCommonWaves * 64 * kPieces * 16);
+        __syncthreads();                                         // the tiles are done with
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) xo[(wave * kPieces + i) * 64 + lane] = piece_of(i);
+        xml[wave * 64 + lane] = make_float2(m_row, l_row);
+        __syncthreads();
+        if (!exists) return;
+        float m_all = -INFINITY, f[KS], l_all = 0.f;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) m_all = fmaxf(m_all, xml[(k * RW + rw) * 64 + lane].x);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            const float2 t2 = xml[(k * RW + rw) * 64 + lane];
+            f[k] = t2.x == -INFINITY ? 0.f : fast_exp2(t2.x - m_all);
+            l_all = fmaf(f[k], t2.y, l_all);
+        }
+#pragma unroll
+        for (int i = 0; i < kPieces / KS; ++i) {
+            const int piece = kw * (kPieces / KS) + i;
+            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const float4 x = xo[((k * RW + rw) * kPieces + piece) * 64 + lane];
+                s.x = fmaf(f[k], x.x, s.x), s.y = fmaf(f[k], x.y, s.y), s.z = fmaf(f[k], x.z, s.z), s.w = fmaf(f[k], x.w, s.w);
+            }
+            o[64 * piece] = s;
+        }
+        if (kw == 0 && h2 == 0) *ml = make_float2(m_all, l_all);
+    }
+}
+
+template <int DT, bool KV8, int D>
+__global__ __launch_bounds__(kCommonThreads, 2) void common_prefix_kernel(const CommonParams p)
+{
+    CommonJob job;
+    int row_waves;
+    if ((int)blockIdx.x < p.p_workgroups) {
+        // workgroups go to XCD (number % 8): the row tiles of one (KV head, range of keys), which read the same tiles, to one
+        const int x = blockIdx.x & 7, w = blockIdx.x >> 3, unit8 = p.by_p_tiles.div(w);
+        const int unit = unit8 * 8 + x, tile = w - unit8 * p.p_tiles;
+        if (unit >= p.p_units) return;
+        const int range = p.by_kv_heads.div(unit);
+        row_waves = p.p_row_waves;
+        job.prefix = true;
+        job.g = unit - range * p.num_kv_heads;
+        job.table = p.prefix_table;
+        job.kbeg = range * p.p_keys;
+        job.kend = min(job.kbeg + p.p_keys, p.prefix_len);
+        job.row0 = tile * 32 * row_waves;
+        job.num_rows = p.rows;
+        job.tok0 = job.pos0 = 0;
+        job.slot = ((int64_t)range * p.num_kv_heads + job.g) * p.p_slots + tile * row_waves;
+    } else {
+        const int i = blockIdx.x - p.p_workgroups, x = i & 7, w = i >> 3, unit8 = p.by_s_tiles.div(w);
+        const int unit = unit8 * 8 + x, tile = w - unit8 * p.s_tiles;
+        if (unit >= p.s_units) return;
+        const int rest = p.by_kv_heads.div(unit), range = p.by_seqs.div(rest), b = rest - range * p.num_seqs;
+        row_waves = p.s_row_waves;
+        job.prefix = false;
+        job.g = unit - rest * p.num_kv_heads;
+        const int cu0 = p.cu_q_lens ? p.cu_q_lens[b] : b, n_b = p.cu_q_lens ? p.cu_q_lens[b + 1] - cu0 : 1;
+        job.row0 = tile * 32 * row_waves;
+        job.num_rows = n_b * p.group;
+        if (job.row0 >= job.num_rows) return;
+        job.tok0 = cu0;
+        job.pos0 = p.context_lens[b] - n_b;
+        // to the position of the tile's last row; the last range takes what there is
+        const int last_row = min(job.row0 + 32 * row_waves, job.num_rows) - 1;
+        job.kbeg = p.prefix_len + range * p.s_keys;
+        job.kend = job.pos0 + p.by_group.div(last_row) + 1;
+        if (range + 1 < p.s_splits) job.kend = min(job.kend, job.kbeg + p.s_keys);
+        if (job.kend <= job.kbeg) return;
+        job.table = p.block_tables + (int64_t)b * p.max_blocks_per_seq;
+        job.slot = p.s_first + ((int64_t)range * p.num_kv_heads + job.g) * p.s_slots + (int)(((int64_t)cu0 * p.group) >> 5) + b + tile * row_waves;
+    }
+    if (row_waves == 4) common_body<DT, KV8, D, 4>(p, job);
+    else if (row_waves == 2) common_body<DT, KV8, D, 2>(p, job);
+    else common_body<DT, KV8, D, 1>(p, job);
+}
+
+// The pieces of 32 rows joined: workgroup (row block x KV head, 32 dims), the pieces dealt to its four waves.
+template <int DT, int D>
+__global__ __launch_bounds__(kCommonThreads) void common_join_kernel(const CommonParams p)
+{
+    constexpr int kPieces = D / 8;
+    __shared__ float4 xo[kCommonWaves][4][64];
+    __shared__ float2 xml[kCommonWaves][64];
+    const int lane = threadIdx.x & 63, n32 = lane & 31, h2 = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tile = p.by_kv_heads.div(blockIdx.x), g = blockIdx.x - tile * p.num_kv_heads, db = blockIdx.y;
+    const int r = 32 * tile + n32, rc = min(r, p.rows - 1), t = p.by_group.div(rc), head = g * p.group + (rc - t * p.group);
+    const TokenPlace at = place_of_token(p, t);
+    // ranges in which the row sees a key
+    const int seen = at.pos + 1, in_prefix = min(seen, p.prefix_len), behind = seen - p.prefix_len;
+    const int np = in_prefix > 0 ? (in_prefix + p.p_keys - 1) / p.p_keys : 0;
+    const int ns = behind > 0 && p.s_splits > 0 ? min((behind + p.s_keys - 1) / p.s_keys, p.s_splits) : 0;
+    // own pieces: this row's place in the first
+    int64_t slot = 0;
+    int own_lane = 0;
+    if (ns > 0) {
+        const int64_t first_row = (int64_t)(p.cu_q_lens ? p.cu_q_lens[at.seq] : at.seq) * p.group;
+        const int in_seq = rc - (int)first_row;
+        slot = p.s_first + (int64_t)g * p.s_slots + (first_row >> 5) + at.seq + (in_seq >> 5);
+        own_lane = in_seq & 31;
+    }
+    const int most = wave_max(np + ns);
+    float m = -INFINITY, l = 0.f;
+    float4 acc[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = wave; i < most; i += kCommonWaves) {
+        if (i >= np + ns) continue;
+        int64_t s = ((int64_t)i * p.num_kv_heads + g) * p.p_slots + tile;
+        int sl = n32;
+        if (i >= np) s = slot + (int64_t)(i - np) * p.num_kv_heads * p.s_slots, sl = own_lane;
+        const float2 t2 = p.ml[s * 32 + sl];
+        const float4* const o = p.o + s * (kPieces * 64) + 4 * db * 64 + sl + 32 * h2;
+        const float m_new = fmaxf(m, t2.x);
+        const float f0 = m == -INFINITY ? 0.f : fast_exp2(m - m_new), f1 = t2.x == -INFINITY ? 0.f : fast_exp2(t2.x - m_new);
+        m = m_new;
+        l = fmaf(f1, t2.y, l * f0);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float4 x = o[64 * j];
+            acc[j].x = fmaf(f1, x.x, acc[j].x * f0), acc[j].y = fmaf(f1, x.y, acc[j].y * f0);
+            acc[j].z = fmaf(f1, x.z, acc[j].z * f0), acc[j].w = fmaf(f1, x.w, acc[j].w * f0);
+        }
+    }
+    xml[wave][lane] = make_float2(m, l);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) xo[wave][j][lane] = acc[j];
+    __syncthreads();
+    // wave w: dims 8w + 4 h2 .. + 3 of the 32
+    float m_all = -INFINITY, l_all = 0.f;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < kCommonWaves; ++k) m_all = fmaxf(m_all, xml[k][lane].x);
+#pragma unroll
+    for (int k = 0; k < kCommonWaves; ++k) {
+        const float2 t2 = xml[k][lane];
+        const float f = t2.x == -INFINITY ? 0.f : fast_exp2(t2.x - m_all);
+        const float4 x = xo[k][wave][lane];
+        l_all = fmaf(f, t2.y, l_all);
+        s.x = fmaf(f, x.x, s.x), s.y = fmaf(f, x.y, s.y), s.z = fmaf(f, x.z, s.z), s.w = fmaf(f, x.w, s.w);
+    }
+    if (r >= p.rows) return;
+    // (a row that sees no key: +0; a sum that is no number stays one)
+    const float inv = l_all == 0.f ? 0.f : (p.v_scales ? p.v_scales[g] : p.out_scale) / l_all;
+    uint2 packed;
+    packed.x = l_all == 0.f ? 0u : narrow2<DT>(s.x * inv, s.y * inv);
+    packed.y = l_all == 0.f ? 0u : narrow2<DT>(s.z * inv, s.w * inv);
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + ((int64_t)t * p.num_heads + head) * D + 32 * db + 8 * wave + 4 * h2) = packed;
+}
+
+}  // namespace optgqa

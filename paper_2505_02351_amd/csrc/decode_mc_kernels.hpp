@@ -28,9 +28,6 @@ namespace optgqa {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kRescaleThreshold = 30.f;    // log2 units: rescale when a tile maximum exceeds the reference by this
-constexpr float kRescaleHeadroom = 60.f;     // ... and then put the reference this far ABOVE the maximum
-constexpr float kNoMax = -1.0e30f;           // "no key seen yet"; finite so that differences stay finite
 constexpr int kMcSteps = 2;                  // steps per wave tile
 #ifndef OPTGQA_RING_TILES
 #define OPTGQA_RING_TILES 3

@@ -1,4 +1,5 @@
-// C ABI of what stands around the attention of a step: rotary positions, rotated cache appends, the verification of drafts.
+// C ABI of a step of drafted tokens behind a common prompt: rotary positions, rotated cache appends, attention with a prefix that
+// all sequences have in common, the verification of drafts.
 // Declarations and the meaning of every argument: include/optgqa.h.
 #include "optgqa.h"
 
@@ -7,6 +8,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "common_prefix_kernels.hpp"
 #include "host.hpp"
 #include "rotary_kernels.hpp"
 #include "verify_kernels.hpp"
@@ -150,6 +152,158 @@ int launch_verify(const VerifyParams& a, int num_seqs, hipStream_t st)
     return rc != OPTGQA_OK ? rc : launch(verify_select_kernel<DT, VEC>, dim3(num_seqs), dim3(kVerifyThreads), 0, st, a);
 }
 
+// How a common-prefix call is cut into pieces; the same for its workspace and its launch.
+struct CommonPlan {
+    int p_row_waves, p_tiles, p_splits, p_keys;
+    int s_row_waves, s_tiles, s_splits, s_keys;
+    int64_t rows, p_slots, s_slots, pieces, p_units, s_units;
+    int64_t workgroups() const { return (p_units + 7) / 8 * 8 * p_tiles + (s_units + 7) / 8 * 8 * s_tiles; }
+    bool fits() const { return rows < (1ll << 31) && workgroups() < (1ll << 31) && p_slots * 4 < (1ll << 31); }
+};
+
+// Row blocks of a workgroup for so many rows: 1, 2 or 4 of 32.
+int common_row_waves(int64_t rows) { return rows > 64 ? 4 : rows > 32 ? 2 : 1; }
+
+// Ranges of `keys` keys: enough for `wanted` workgroups of `units`, none shorter than two tiles of 32 for each key group of the workgroup.
+void common_ranges(int64_t keys, int64_t units, int64_t wanted, int64_t at_most, int row_waves, int& splits, int& range)
+{
+    const int64_t step = 32 * (kCommonWaves / row_waves);
+    int64_t n = std::max<int64_t>(std::min<int64_t>(wanted / std::max<int64_t>(units, 1), keys / (2 * step)), (keys + at_most - 1) / at_most);
+    n = std::max<int64_t>(n, 1);
+    const int64_t each = ((keys + n - 1) / n + step - 1) / step * step;
+    range = (int)each;
+    splits = (int)((keys + each - 1) / each);
+}
+
+CommonPlan plan_common(int64_t num_tokens, int64_t num_seqs, int num_heads, int num_kv_heads, int64_t prefix_len, int64_t max_context_len, int64_t max_q_len)
+{
+    const int64_t group = num_heads / num_kv_heads;
+    CommonPlan c{};
+    c.rows = num_tokens * group;
+    c.p_slots = (c.rows + 31) / 32;
+    c.s_slots = c.rows / 32 + num_seqs;                          // a sequence's first: its first row / 32 + its number
+    c.p_row_waves = common_row_waves(c.rows);
+    c.p_tiles = 1, c.p_keys = c.s_keys = 32, c.s_tiles = 1;
+    if (prefix_len > 0) {
+        c.p_tiles = (int)((c.p_slots + c.p_row_waves - 1) / c.p_row_waves);
+        common_ranges(prefix_len, (int64_t)num_kv_heads * c.p_tiles, 2 * num_cus(), prefix_len, c.p_row_waves, c.p_splits, c.p_keys);
+    }
+    const int64_t behind = max_context_len - prefix_len, own_rows = std::min(max_q_len, num_tokens) * group;
+    c.s_row_waves = common_row_waves(own_rows);
+    if (behind > 0) {
+        c.s_tiles = (int)((own_rows + 32 * c.s_row_waves - 1) / (32 * c.s_row_waves));
+        common_ranges(behind, num_seqs * num_kv_heads * c.s_tiles, 2 * num_cus(), 1024, c.s_row_waves, c.s_splits, c.s_keys);
+    }
+    c.p_units = (int64_t)num_kv_heads * c.p_splits;
+    c.s_units = num_seqs * num_kv_heads * c.s_splits;
+    c.pieces = num_kv_heads * (c.p_splits * c.p_slots + c.s_splits * c.s_slots);
+    return c;
+}
+
+size_t common_bytes(const CommonPlan& c, int head_dim) { return (size_t)c.pieces * 32 * (head_dim * sizeof(float) + sizeof(float2)); }
+
+template <int DT, bool KV8, int D>
+int launch_common(const CommonParams& p, int workgroups, hipStream_t st)
+{
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&common_prefix_kernel<DT, KV8, D>),
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, kCommonLds<D>);
+    if (attr != hipSuccess) return OPTGQA_ERR_LAUNCH;
+    if (workgroups > 0) {
+        const int rc = launch(common_prefix_kernel<DT, KV8, D>, dim3(workgroups), dim3(kCommonThreads), kCommonLds<D>, st, p);
+        if (rc != OPTGQA_OK) return rc;
+    }
+    return launch(common_join_kernel<DT, D>, dim3(p.p_slots * p.num_kv_heads, D / 32), dim3(kCommonThreads), 0, st, p);
+}
+
+template <int DT, bool KV8>
+int launch_common_d(const CommonParams& p, int head_dim, int workgroups, hipStream_t st)
+{
+    return head_dim == 128 ? launch_common<DT, KV8, 128>(p, workgroups, st) : launch_common<DT, KV8, 64>(p, workgroups, st);
+}
+
+int common_impl(void* out, const void* q, const void* k_cache, const void* v_cache, const int32_t* prefix_table,
+                const int32_t* block_tables, const int32_t* context_lens, const int32_t* cu_q_lens, const float* alibi_slopes, float scale,
+                int num_tokens, int num_seqs, int num_heads, int num_kv_heads, int head_dim, int block_size, int num_prefix_blocks,
+                int max_blocks_per_seq, int max_context_len, int max_q_len, void* workspace, size_t workspace_bytes, int dtype,
+                const KvScales* scales, void* stream)
+{
+    if (num_tokens < 0 || num_seqs < 0 || num_heads <= 0 || num_kv_heads <= 0 || head_dim <= 0 || block_size <= 0 || num_prefix_blocks < 0 ||
+        max_blocks_per_seq < 0 || max_context_len < 0 || max_q_len < 0)
+        return OPTGQA_ERR_SHAPE;
+    if (!std::isfinite(scale) || num_heads % num_kv_heads || num_heads > 65535) return OPTGQA_ERR_SHAPE;
+    if (!dtype_ok(dtype) || !head_dim_ok(head_dim) || !block_size_ok(block_size)) return OPTGQA_ERR_UNSUPPORTED;
+    const int64_t prefix_len = (int64_t)num_prefix_blocks * block_size;
+    if (max_context_len > (int64_t)max_blocks_per_seq * block_size && max_context_len > prefix_len) return OPTGQA_ERR_SHAPE;
+    if (prefix_len > (1ll << 30) || max_context_len > (1 << 30)) return OPTGQA_ERR_SHAPE;
+    if (scales && scales->per_head() && !scales->v_heads) return OPTGQA_ERR_NULL;
+    if (scales && !scales->valid()) return OPTGQA_ERR_SHAPE;
+    if (num_tokens == 0) return OPTGQA_OK;
+    if (num_seqs == 0 || (!cu_q_lens && num_tokens != num_seqs)) return OPTGQA_ERR_SHAPE;
+    if (max_q_len == 0) return OPTGQA_ERR_SHAPE;
+    if (!out || !q || !k_cache || !v_cache || !context_lens || (num_prefix_blocks && !prefix_table) || (max_context_len > prefix_len && !block_tables))
+        return OPTGQA_ERR_NULL;
+    if (!aligned16(out) || !aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache)) return OPTGQA_ERR_UNSUPPORTED;
+    const CommonPlan c = plan_common(num_tokens, num_seqs, num_heads, num_kv_heads, prefix_len, max_context_len, cu_q_lens ? max_q_len : 1);
+    if (!c.fits()) return OPTGQA_ERR_SHAPE;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < common_bytes(c, head_dim)) return OPTGQA_ERR_WORKSPACE;
+
+    CommonParams p;
+    p.out = out;
+    p.q = q;
+    p.k_cache = k_cache;
+    p.v_cache = v_cache;
+    p.prefix_table = prefix_table;
+    p.block_tables = block_tables;
+    p.context_lens = context_lens;
+    p.cu_q_lens = cu_q_lens;
+    p.slopes = alibi_slopes;
+    p.scale2 = prefill_scale2(scale);                            // (the bias rides in the scores here too)
+    p.out_scale = 1.f;
+    p.k_scales = p.v_scales = nullptr;
+    if (scales && scales->per_head()) {
+        p.k_scales = scales->k_heads;
+        p.v_scales = scales->v_heads;
+    } else if (scales) {
+        p.scale2 *= scales->k;
+        p.out_scale = scales->v;
+    }
+    p.num_tokens = num_tokens;
+    p.num_seqs = num_seqs;
+    p.num_heads = num_heads;
+    p.num_kv_heads = num_kv_heads;
+    p.group = num_heads / num_kv_heads;
+    p.block_shift = __builtin_ctz(block_size);
+    p.max_blocks_per_seq = max_blocks_per_seq;
+    p.prefix_len = (int)prefix_len;
+    p.rows = (int)c.rows;
+    p.p_row_waves = c.p_row_waves;
+    p.p_tiles = c.p_tiles;
+    p.p_splits = c.p_splits;
+    p.p_keys = c.p_keys;
+    p.p_units = (int)c.p_units;
+    p.p_workgroups = (int)((c.p_units + 7) / 8 * 8 * c.p_tiles);
+    p.s_row_waves = c.s_row_waves;
+    p.s_tiles = c.s_tiles;
+    p.s_splits = c.s_splits;
+    p.s_keys = c.s_keys;
+    p.s_units = (int)c.s_units;
+    p.p_slots = (int)c.p_slots;
+    p.s_slots = (int)c.s_slots;
+    p.s_first = c.p_splits * num_kv_heads * c.p_slots;
+    p.o = static_cast<float4*>(workspace);
+    p.ml = reinterpret_cast<float2*>(static_cast<unsigned char*>(workspace) + (size_t)c.pieces * 32 * head_dim * sizeof(float));
+    p.by_group.set((uint32_t)p.group);
+    p.by_p_tiles.set((uint32_t)c.p_tiles);
+    p.by_s_tiles.set((uint32_t)c.s_tiles);
+    p.by_kv_heads.set((uint32_t)num_kv_heads);
+    p.by_seqs.set((uint32_t)num_seqs);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int workgroups = (int)c.workgroups();
+    if (dtype == OPTGQA_F16)
+        return scales ? launch_common_d<kF16, true>(p, head_dim, workgroups, st) : launch_common_d<kF16, false>(p, head_dim, workgroups, st);
+    return scales ? launch_common_d<kBF16, true>(p, head_dim, workgroups, st) : launch_common_d<kBF16, false>(p, head_dim, workgroups, st);
+}
+
 }  // namespace
 
 static_assert(kF16 == OPTGQA_F16 && kBF16 == OPTGQA_BF16 && kF32 == OPTGQA_F32, "the header's values");
@@ -287,6 +441,54 @@ int optgqa_verify_drafts(int64_t* tokens, int32_t* num_accepted, const void* tar
     if (dtype == OPTGQA_F32) return wide ? launch_verify<kF32, 4>(a, num_seqs, st) : launch_verify<kF32, 1>(a, num_seqs, st);
     if (dtype == OPTGQA_F16) return wide ? launch_verify<kF16, 8>(a, num_seqs, st) : launch_verify<kF16, 1>(a, num_seqs, st);
     return wide ? launch_verify<kBF16, 8>(a, num_seqs, st) : launch_verify<kBF16, 1>(a, num_seqs, st);
+}
+
+size_t optgqa_common_prefix_workspace_bytes(int num_tokens, int num_seqs, int num_heads, int num_kv_heads, int head_dim,
+                                            int block_size, int num_prefix_blocks, int max_context_len, int max_q_len)
+{
+    if (num_tokens <= 0 || num_seqs <= 0 || num_heads <= 0 || num_kv_heads <= 0 || num_heads % num_kv_heads || !head_dim_ok(head_dim) ||
+        !block_size_ok(block_size) || num_prefix_blocks < 0 || max_context_len < 0 || max_q_len <= 0)
+        return 0;
+    const CommonPlan c = plan_common(num_tokens, num_seqs, num_heads, num_kv_heads, (int64_t)num_prefix_blocks * block_size, max_context_len, max_q_len);
+    // (without prefix sums of new tokens a sequence has one, whatever the bound: the call needs the larger of the two)
+    const CommonPlan one = plan_common(num_tokens, num_seqs, num_heads, num_kv_heads, (int64_t)num_prefix_blocks * block_size, max_context_len, 1);
+    return std::max<size_t>(std::max(common_bytes(c, head_dim), common_bytes(one, head_dim)), 16);
+}
+
+int optgqa_paged_attention_common(void* out, const void* q, const void* k_cache, const void* v_cache, const int32_t* prefix_table,
+                                  const int32_t* block_tables, const int32_t* context_lens, const int32_t* cu_q_lens,
+                                  const float* alibi_slopes, float scale, int num_tokens, int num_seqs, int num_heads, int num_kv_heads,
+                                  int head_dim, int block_size, int num_prefix_blocks, int max_blocks_per_seq, int max_context_len,
+                                  int max_q_len, void* workspace, size_t workspace_bytes, int dtype, void* stream)
+{
+    return common_impl(out, q, k_cache, v_cache, prefix_table, block_tables, context_lens, cu_q_lens, alibi_slopes, scale, num_tokens, num_seqs,
+                       num_heads, num_kv_heads, head_dim, block_size, num_prefix_blocks, max_blocks_per_seq, max_context_len, max_q_len, workspace,
+                       workspace_bytes, dtype, nullptr, stream);
+}
+
+int optgqa_paged_attention_common_fp8(void* out, const void* q, const void* k_cache, const void* v_cache, const int32_t* prefix_table,
+                                  const int32_t* block_tables, const int32_t* context_lens, const int32_t* cu_q_lens,
+                                  const float* alibi_slopes, float scale, float k_scale, float v_scale, int num_tokens, int num_seqs, int num_heads, int num_kv_heads,
+                                  int head_dim, int block_size, int num_prefix_blocks, int max_blocks_per_seq, int max_context_len,
+                                  int max_q_len, void* workspace, size_t workspace_bytes, int dtype, void* stream)
+{
+    const KvScales scales{k_scale, v_scale, nullptr, nullptr};
+    return common_impl(out, q, k_cache, v_cache, prefix_table, block_tables, context_lens, cu_q_lens, alibi_slopes, scale, num_tokens, num_seqs,
+                       num_heads, num_kv_heads, head_dim, block_size, num_prefix_blocks, max_blocks_per_seq, max_context_len, max_q_len, workspace,
+                       workspace_bytes, dtype, &scales, stream);
+}
+
+int optgqa_paged_attention_common_fp8_heads(void* out, const void* q, const void* k_cache, const void* v_cache, const int32_t* prefix_table,
+                                  const int32_t* block_tables, const int32_t* context_lens, const int32_t* cu_q_lens,
+                                  const float* alibi_slopes, float scale, const float* k_scales, const float* v_scales, int num_tokens, int num_seqs, int num_heads, int num_kv_heads,
+                                  int head_dim, int block_size, int num_prefix_blocks, int max_blocks_per_seq, int max_context_len,
+                                  int max_q_len, void* workspace, size_t workspace_bytes, int dtype, void* stream)
+{
+    if (!k_scales || !v_scales) return OPTGQA_ERR_NULL;
+    const KvScales scales{0.f, 0.f, k_scales, v_scales};
+    return common_impl(out, q, k_cache, v_cache, prefix_table, block_tables, context_lens, cu_q_lens, alibi_slopes, scale, num_tokens, num_seqs,
+                       num_heads, num_kv_heads, head_dim, block_size, num_prefix_blocks, max_blocks_per_seq, max_context_len, max_q_len, workspace,
+                       workspace_bytes, dtype, &scales, stream);
 }
 
 }  // extern "C"

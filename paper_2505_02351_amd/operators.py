@@ -1,5 +1,5 @@
-"""Binding of the calls that stand around the attention of a step: rotary positions, rotated cache appends and the
-verification of drafted tokens.
+"""Binding of the calls that stand around the attention of a step: rotary positions, rotated cache appends, the
+attention of a batch with a common prefix and the verification of drafted tokens.
 
 Conventions as in the package: q [T, Hq, D], k and v [T, Hkv, D] with any token stride (dense in their
 last two dims: slices of one projection's rows will do), caches [NB, Hkv, bs, D], positions [T] int32,
@@ -27,12 +27,16 @@ def declare(lib: ctypes.CDLL) -> None:
         "rotary_and_cache": [vp] * 9 + [i32] * 6 + [f32, i32] + [i64] * 4 + [i32, vp],
         "rotary_and_cache_fp8": [vp] * 9 + [i32] * 6 + [f32, i32] + [i64] * 4 + [f32, f32, i32, vp],
         "rotary_and_cache_fp8_heads": [vp] * 9 + [i32] * 6 + [f32, i32] + [i64] * 4 + [vp, vp, i32, vp],
+        "paged_attention_common": [vp] * 9 + [f32] + [i32] * 10 + [vp, ctypes.c_size_t, i32, vp],
+        "paged_attention_common_fp8": [vp] * 9 + [f32] * 3 + [i32] * 10 + [vp, ctypes.c_size_t, i32, vp],
+        "paged_attention_common_fp8_heads": [vp] * 9 + [f32, vp, vp] + [i32] * 10 + [vp, ctypes.c_size_t, i32, vp],
         "verify_drafts": [vp] * 8 + [i32] * 3 + [i64, i64, vp, ctypes.c_size_t, i32, vp],
     }.items():
         f = getattr(lib, "optgqa_" + name)
         f.restype, f.argtypes = i32, args
-    f = lib.optgqa_verify_drafts_workspace_bytes
-    f.restype, f.argtypes = ctypes.c_size_t, [i32, i32]
+    for name, n in (("common_prefix_workspace_bytes", 9), ("verify_drafts_workspace_bytes", 2)):
+        f = getattr(lib, "optgqa_" + name)
+        f.restype, f.argtypes = ctypes.c_size_t, [i32] * n
 
 
 def rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: int = ROTARY_PLAIN, factor: float = 1.0,
@@ -139,6 +143,67 @@ def rotary_and_cache_fp8_heads(q_out: torch.Tensor, q: torch.Tensor, k: torch.Te
     _pkg._head_scales(q, k_cache, k_scales, v_scales)
     _append("optgqa_rotary_and_cache_fp8_heads", q_out, q, k, v, k_cache, v_cache, slot_mapping, positions, freqs, interleaved, magnitude,
             stream, True, (k_scales.data_ptr(), v_scales.data_ptr()))
+
+
+def common_prefix_workspace_bytes(num_tokens: int, num_seqs: int, num_heads: int, num_kv_heads: int, head_dim: int, block_size: int,
+                                  num_prefix_blocks: int, max_context_len: int, max_q_len: int = 1) -> int:
+    """optgqa_common_prefix_workspace_bytes."""
+    return int(_pkg.load_library().optgqa_common_prefix_workspace_bytes(num_tokens, num_seqs, num_heads, num_kv_heads, head_dim, block_size,
+                                                                        num_prefix_blocks, max_context_len, max_q_len))
+
+
+def _common(name, out, q, k_cache, v_cache, prefix_table, block_tables, context_lens, cu_q_lens, alibi_slopes, scale, max_context_len,
+            max_q_len, workspace, stream, kv8, scales) -> None:
+    lib = _pkg.load_library()
+    _pkg._attn_typed(q, out, k_cache, v_cache, block_tables, context_lens, alibi_slopes, kv8=kv8, cu_q_lens=cu_q_lens)
+    _pkg._typed(q, i32=(("prefix_table", prefix_table),))
+    T, Hq, D = q.shape
+    NB, Hkv, bs, Dk = k_cache.shape
+    B = context_lens.shape[0]
+    if (Dk != D or out.shape != q.shape or v_cache.shape != k_cache.shape or prefix_table.dim() != 1 or block_tables.dim() != 2
+            or block_tables.shape[0] != B or (T != B if cu_q_lens is None else cu_q_lens.shape != (B + 1,))
+            or (alibi_slopes is not None and alibi_slopes.shape != (Hq,))):
+        raise ValueError("optgqa: shape mismatch between q, out, the tables, lengths, slopes and the caches")
+    for t, n in ((out, "out"), (q, "q"), (k_cache, "k_cache"), (v_cache, "v_cache"), (prefix_table, "prefix_table"),
+                 (block_tables, "block_tables"), (context_lens, "context_lens"), (cu_q_lens, "cu_q_lens"), (alibi_slopes, "alibi_slopes")):
+        if t is not None:
+            _pkg._dense(t, n)
+    ws_bytes = _pkg._workspace(workspace, q)
+    rc = getattr(lib, name)(out.data_ptr(), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), prefix_table.data_ptr(),
+                            block_tables.data_ptr(), context_lens.data_ptr(), _pkg._ptr(cu_q_lens), _pkg._ptr(alibi_slopes), scale, *scales,
+                            T, B, Hq, Hkv, D, bs, prefix_table.shape[0], block_tables.shape[1], max_context_len, max_q_len,
+                            _pkg._ptr(workspace), ws_bytes, _pkg._dtype_code(q), _pkg._stream(stream))
+    _pkg._check(rc, name)
+
+
+def paged_attention_common(out: torch.Tensor, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, prefix_table: torch.Tensor,
+                           block_tables: torch.Tensor, context_lens: torch.Tensor, cu_q_lens: Optional[torch.Tensor],
+                           alibi_slopes: Optional[torch.Tensor], scale: float, max_context_len: int, max_q_len: int = 1,
+                           workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """optgqa_paged_attention_common: attention of each sequence's new tokens over a prefix that all sequences have in common
+    (prefix_table [blocks] int32) and their own blocks behind it; cu_q_lens None: one new token each."""
+    _common("optgqa_paged_attention_common", out, q, k_cache, v_cache, prefix_table, block_tables, context_lens, cu_q_lens, alibi_slopes,
+            scale, max_context_len, max_q_len, workspace, stream, False, ())
+
+
+def paged_attention_common_fp8(out: torch.Tensor, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, prefix_table: torch.Tensor,
+                               block_tables: torch.Tensor, context_lens: torch.Tensor, cu_q_lens: Optional[torch.Tensor],
+                               alibi_slopes: Optional[torch.Tensor], scale: float, k_scale: float, v_scale: float, max_context_len: int,
+                               max_q_len: int = 1, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """optgqa_paged_attention_common_fp8: the same over E4M3 caches (uint8 tensors), one scale per tensor."""
+    _common("optgqa_paged_attention_common_fp8", out, q, k_cache, v_cache, prefix_table, block_tables, context_lens, cu_q_lens, alibi_slopes,
+            scale, max_context_len, max_q_len, workspace, stream, True, (float(k_scale), float(v_scale)))
+
+
+def paged_attention_common_fp8_heads(out: torch.Tensor, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                                     prefix_table: torch.Tensor, block_tables: torch.Tensor, context_lens: torch.Tensor,
+                                     cu_q_lens: Optional[torch.Tensor], alibi_slopes: Optional[torch.Tensor], scale: float,
+                                     k_scales: torch.Tensor, v_scales: torch.Tensor, max_context_len: int, max_q_len: int = 1,
+                                     workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """optgqa_paged_attention_common_fp8_heads: the same with one scale pair per KV head (float32 device tensors [Hkv])."""
+    _pkg._head_scales(q, k_cache, k_scales, v_scales)
+    _common("optgqa_paged_attention_common_fp8_heads", out, q, k_cache, v_cache, prefix_table, block_tables, context_lens, cu_q_lens,
+            alibi_slopes, scale, max_context_len, max_q_len, workspace, stream, True, (k_scales.data_ptr(), v_scales.data_ptr()))
 
 
 _PROBABILITIES = {torch.float16: _pkg.F16, torch.bfloat16: _pkg.BF16, torch.float32: 2}

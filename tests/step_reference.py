@@ -66,3 +66,37 @@ def verify(target, draft, draft_tokens, cu, accept_u, sample_u, width):
         tokens[b, n] = np.argmax(over) if over.any() else -1
         accepted[b] = n
     return tokens, accepted
+
+
+def attend(q, keys, values, positions, slopes, scale):
+    """Rows q [n, Hq, D] at `positions` over keys, values [L, Hkv, D] up to each row's position -> (out, what the weights
+    average: sum of weight * |value|).  A row that sees no key is 0."""
+    n, Hq, D = q.shape
+    L, Hkv, _ = keys.shape
+    out, size = np.zeros((n, Hq, D)), np.zeros((n, Hq, D))
+    for i in range(n):
+        see = int(min(max(positions[i] + 1, 0), L))
+        if see == 0:
+            continue
+        for h in range(Hq):
+            g = h // (Hq // Hkv)
+            s = scale * (keys[:see, g] @ q[i, h])
+            if slopes is not None:
+                s = s + slopes[h] * (np.arange(see) - positions[i])
+            w = np.exp(s - s.max())
+            w /= w.sum()
+            out[i, h] = w @ values[:see, g]
+            size[i, h] = w @ np.abs(values[:see, g])
+    return out, size
+
+
+# Relative error of a softmax weight in the kernels: rounded to fp16 once, or kept to 16 bits as two bf16; and 1.2e-4 for the
+# score (128 products summed in 32 bits, of magnitudes that add up to some 10: 128 * 10 * 2^-24, with the exponential's
+# argument and value).
+WEIGHT = {"f16": 2.0 ** -11 + 1.2e-4, "bf16": 2.0 ** -16 + 1.2e-4}
+
+
+def attention_bar(ref, size, dtype):
+    """What a kernel's output may differ from attend()'s: weights off by WEIGHT on both sides of the quotient, one rounding."""
+    slack = WEIGHT[dtype] * (size + np.abs(ref))
+    return half_step(np.abs(ref) + slack, EPS[dtype], SMALLEST[dtype]) + slack

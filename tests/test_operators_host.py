@@ -126,3 +126,44 @@ def test_verification_refuses_before_any_launch(G):
         assert v(**{name: ctypes.c_void_p(at)}) == -3, name
     assert v(ws=None) == -4 and v(wsb=need - 1) == -4 and v(ws=ctypes.c_void_p(8)) == -4
     assert v(B=0, tokens=None) == 0
+
+
+def test_common_prefix_refuses_before_any_launch(G):
+    lib = G.load_library()
+    need = G.common_prefix_workspace_bytes(8, 4, 8, 2, 64, 16, 16, 320, 3)
+    assert need > 0
+    for kw in (dict(T=0), dict(B=0), dict(Hq=7), dict(D=96), dict(bs=8), dict(NP=-1), dict(Lmax=-1), dict(n=0)):
+        a = {**dict(T=8, B=4, Hq=8, Hkv=2, D=64, bs=16, NP=16, Lmax=320, n=3), **kw}
+        assert G.common_prefix_workspace_bytes(a["T"], a["B"], a["Hq"], a["Hkv"], a["D"], a["bs"], a["NP"], a["Lmax"], a["n"]) == 0, kw
+
+    def c(call=lib.optgqa_paged_attention_common, scales=(), out=ONE, q=ONE, kc=ONE, vc=ONE, pt=ONE, bt=ONE, cl=ONE, cu=ONE, scale=0.1, T=8, B=4,
+          Hq=8, Hkv=2, D=64, bs=16, NP=16, MB=20, Lmax=320, n=3, ws=ONE, wsb=None, dt=0):
+        return call(out, q, kc, vc, pt, bt, cl, cu, None, scale, *scales, T, B, Hq, Hkv, D, bs, NP, MB, Lmax, n, ws, need if wsb is None else wsb, dt, None)
+
+    one, heads = lib.optgqa_paged_attention_common_fp8, lib.optgqa_paged_attention_common_fp8_heads
+    for call, scales in ((lib.optgqa_paged_attention_common, ()), (one, (1.0, 1.0)), (heads, (ONE, ONE))):
+        def a(**kw):
+            return c(call, scales, **kw)
+        assert a(T=-1) == -2 and a(B=-1) == -2 and a(Hq=7) == -2 and a(Hq=0) == -2 and a(Hkv=0) == -2 and a(NP=-1) == -2 and a(Lmax=-1) == -2
+        assert a(n=-1) == -2 and a(n=0) == -2 and a(B=0) == -2 and a(MB=19) == -2 and a(Hq=70000, Hkv=70000) == -2
+        assert a(scale=float("nan")) == -2 and a(scale=float("inf")) == -2
+        assert a(D=96) == -3 and a(bs=8) == -3 and a(dt=2) == -3 and a(dt=-1) == -3
+        for name in ("out", "q", "kc", "vc", "pt", "bt", "cl"):
+            assert a(**{name: None}) == -1, name
+        for name in ("out", "q", "kc", "vc"):
+            assert a(**{name: ctypes.c_void_p(8)}) == -3, name
+        assert a(cu=None) == -2                                  # 8 tokens of 4 sequences
+        assert a(ws=None) == -4 and a(wsb=need - 1) == -4 and a(ws=ctypes.c_void_p(8)) == -4
+        assert a(T=0, q=None) == 0
+        assert a(T=2**30, Hq=64, Hkv=2) == -2                    # 2^35 rows
+        assert a(NP=2**27, Lmax=100) == -2
+    for bad in (0.0, -1.0, float("nan"), float("inf")):
+        assert c(one, (bad, 1.0)) == -2 and c(one, (1.0, bad)) == -2
+    assert c(heads, (None, ONE)) == -1 and c(heads, (ONE, None)) == -1
+
+
+def test_common_prefix_workspace_covers_every_smaller_call(G):
+    """Sized by bounds: a call with one new token a sequence fits what its drafts' bound asks for."""
+    for T, B, Hq, Hkv, D, NP, Lmax, n in ((9, 9, 32, 8, 128, 100, 5000, 9), (64, 64, 32, 4, 128, 0, 4000, 5), (600, 64, 8, 8, 64, 1000, 20000, 100)):
+        big = G.common_prefix_workspace_bytes(T, B, Hq, Hkv, D, 16, NP, Lmax, n)
+        assert big >= G.common_prefix_workspace_bytes(T, B, Hq, Hkv, D, 16, NP, Lmax, 1)
