@@ -55,27 +55,45 @@ template <int D> constexpr int kCommonLds = [] {
     return tiles > join ? tiles : join;
 }();
 
-// The sequence of token t and the token's position in it; seq < 0: no sequence has it.  All lanes of a wave together, a
-// sequence's end a lane, 64 at a time.
-struct TokenPlace { int seq, pos; };
-__device__ __forceinline__ TokenPlace place_of_token(const CommonParams& p, int t)
-{
-    if (!p.cu_q_lens) return {t, p.context_lens[t] - 1};
-    const int lane = threadIdx.x & 63;
-    int b = 0;
-    for (int first = 0; first < p.num_seqs; first += 64) {
-        const int n = min(p.num_seqs - first, 64);
-        const int end = p.cu_q_lens[first + min(lane, n - 1) + 1];
-        int k = 0;                                               // of the n sequences, those that end at or before t
-#pragma unroll
-        for (int s = 32; s; s >>= 1)
-            if (k + s <= n && __shfl(end, k + s - 1) <= t) k += s;
-        if (k + 1 <= n && __shfl(end, k) <= t) ++k;
-        b += k;
+// The sequence of token t (seq < 0: none has it), its context length and the token behind its last.  All lanes of a wave
+// together: first the guess that every sequence has one new token, which one round trip to memory confirms, else the sequences'
+// ends and lengths, 64 at a time, one a lane.
+struct TokenPlace {
+    int seq, len, end;
+    __device__ __forceinline__ int pos(int t) const { return seq < 0 ? -1 : len - end + t; }
+};
+// What the guess needs, asked for here and used by find() (so that other loads can be asked for in between).
+struct PlaceGuess {
+    int seq, first, end, len;   // seq: the t-th, or the last
+    __device__ __forceinline__ PlaceGuess(const CommonParams& p, int t)
+    {
+        seq = min(t, p.num_seqs - 1);
+        first = seq, end = seq + 1;
+        if (p.cu_q_lens) first = p.cu_q_lens[seq], end = p.cu_q_lens[seq + 1];
+        len = p.context_lens[seq];
     }
-    if (b >= p.num_seqs) return {-1, -1};
-    return {b, p.context_lens[b] - p.cu_q_lens[b + 1] + t};
-}
+    __device__ __forceinline__ TokenPlace find(const CommonParams& p, int t) const
+    {
+        if (__builtin_amdgcn_ballot_w64(first != t || end != t + 1) == 0) return {seq, len, end};
+        const int lane = threadIdx.x & 63;
+        TokenPlace at{-1, 0, 0};
+        for (int from = 0; from < p.num_seqs; from += 64) {
+            const int n = min(p.num_seqs - from, 64), b = from + min(lane, n - 1);
+            const int ends = p.cu_q_lens[b + 1], lens = p.context_lens[b];
+            int k = 0;                                           // of the n sequences, those that end at or before t
+#pragma unroll
+            for (int s = 32; s; s >>= 1) {
+                const int e = __shfl(ends, (k + s - 1) & 63);    // (all lanes exchange, also those that do not want it)
+                if (k + s <= n && e <= t) k += s;
+            }
+            const int next = __shfl(ends, k & 63);
+            if (k + 1 <= n && next <= t) ++k;
+            const int e = __shfl(ends, k & 63), l = __shfl(lens, k & 63);
+            if (at.seq < 0 && k < n) at = {from + k, l, e};
+        }
+        return at;
+    }
+};
 
 // A workgroup's rows and keys.
 struct CommonJob {
@@ -86,6 +104,7 @@ struct CommonJob {
     int row0, num_rows;         // its first row, of the batch's (prefix) or of the sequence's
     int tok0, pos0;             // token and position of row 0 (pos0: own parts)
     int64_t slot;               // piece of its first 32 rows
+    int held_first, held;       // the lane's entry of `table`: held_first + lane
 };
 
 template <int DT> __device__ __forceinline__ bool any_not_finite(uint4 x)
@@ -126,6 +145,20 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rw = wave % RW, kw = wave / RW;
     const int kbeg = job.kbeg, kend = job.kend;
     const int ntiles = (kend - kbeg + kPfKeys - 1) / kPfKeys, steps = (ntiles + KS - 1) / KS;
+    // ---- the lane's row, its query and what its position is made of: asked for in front of everything that is waited for -----
+    const int r = job.row0 + 32 * rw + n32;
+    const bool row_ok = r < job.num_rows;
+    const int rc = min(r, job.num_rows - 1), ti = p.by_group.div(rc), head = job.g * p.group + (rc - ti * p.group);
+    const int t = job.tok0 + ti;
+    uint4 qb[kQ];
+    {
+        const unsigned char* const qp = static_cast<const unsigned char*>(p.q) + ((int64_t)t * p.num_heads + head) * (D * 2) + 16 * h2;
+#pragma unroll
+        for (int m = 0; m < kQ; ++m) qb[m] = *reinterpret_cast<const uint4*>(qp + 32 * m);
+    }
+    float slope = p.slopes ? p.slopes[head] : 0.f;
+    int pos = job.pos0 + ti;
+    if (job.prefix) pos = PlaceGuess(p, t).find(p, t).pos(t);
     auto has = [&](int j) __attribute__((always_inline)) { return j * KS + kw < ntiles; };
 
     // ---- where tiles come from: a lane holds one of 64 block numbers -------------------------------------
@@ -135,16 +168,16 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
     const unsigned char* const kc = static_cast<const unsigned char*>(p.k_cache) + head_bytes;
     const unsigned char* const vc = static_cast<const unsigned char*>(p.v_cache) + head_bytes;
     const int last_block = (kend - 1) >> bshift;
-    int held_first = kbeg >> bshift;
-    int held = job.table[min(held_first + lane, last_block)];
+    int held_first = job.held_first, held = job.held;
     const int load_row = Tile::load_row(lane), load_col = Tile::load_col(lane);
     const uint32_t lane_off = (uint32_t)(load_row * D * ES + 8 * load_col * ES);
     // byte offset, in either cache from its KV head's first block on, of key `key` (wave-uniform)
     auto key_at = [&](int key) __attribute__((always_inline)) -> uint64_t {
         const int block = key >> bshift;
         if (__builtin_expect(block - held_first >= 64, 0)) {
-            held_first = block;
+            held_first = block - 8;                              // (V tiles follow K tiles by a step: up to 64 keys)
             held = job.table[min(held_first + lane, last_block)];
+            asm volatile("" : "+v"(held));                       // (waited for here, not on the way that reads no table)
         }
         return (uint64_t)(uint32_t)__builtin_amdgcn_readlane(held, block - held_first) * blk_bytes + (uint32_t)((key & bmask) * (D * ES));
     };
@@ -188,25 +221,37 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
             *reinterpret_cast<uint4*>(lds + at + (rw * kWaveGroups + n) * Tile::kGroup + 16 * lane) = widen8_e4m3<DT>(stage[n][0], stage[n][1]);
     };
 
-    // ---- the lane's row ---------------------------------------------------------------------------------
-    const int r = job.row0 + 32 * rw + n32;
-    const bool row_ok = r < job.num_rows;
-    const int rc = min(r, job.num_rows - 1), ti = p.by_group.div(rc), head = job.g * p.group + (rc - ti * p.group);
-    const int t = job.tok0 + ti;
-    const int pos = job.prefix ? place_of_token(p, t).pos : job.pos0 + ti;
+    // ---- the first tiles -------------------------------------------------------------------------------------
+    // RW > 1: a key group's K and V tiles in rings of NBUF buffers.  The scores of a step's tile are made a step ahead, under the
+    // softmax of the tile before, so K tiles run one ahead of V tiles: step j asks for K tile j + 1 + kLead and V tile j + kLead.
+    // RW == 1: a wave's own tiles, one buffer: the next K tile is asked for when this one's scores are there, the next V
+    // tile when this one's output is.
+    constexpr int kLead = NBUF / 2;
+    constexpr int kLoads = 2 * kWaveGroups;                      // of a wave, per K and V tile
+    auto buffer_v = [&](int j) __attribute__((always_inline)) { return buffer(j) + Tile::kTile; };
+    const int at_k = buffer(0), at_v = at_k + Tile::kTile;       // (RW == 1)
+    auto ask_k = [&](int j) __attribute__((always_inline)) { if (has(j)) ask(runs_of(j), kc, buffer(j)); };
+    auto ask_v = [&](int j) __attribute__((always_inline)) { if (has(j)) ask(runs_of(j), vc, buffer_v(j)); };
+    asm volatile("" : "+v"(held) :: "memory");
+    if constexpr (KV8) {
+        if (has(0)) {
+            const Runs first = runs_of(0);
+            fetch(first, kc, stage_k);
+            fetch(first, vc, stage_v);
+        }
+    } else {
+        ask_k(0);
+        if constexpr (RW > 1) ask_k(1);
+        ask_v(0);
+        if constexpr (RW > 1 && kLead == 2) ask_k(2), ask_v(1);
+    }
     const int lim = row_ok ? min(pos + 1, kend) : kend;          // keys below it are visible
     const int least = -wave_max(-lim);                           // tiles that end at or below it need no mask
-    uint4 qb[kQ];
-    {
-        const unsigned char* const qp = static_cast<const unsigned char*>(p.q) + ((int64_t)t * p.num_heads + head) * (D * 2) + 16 * h2;
+    const uint32_t keep_q = row_ok ? 0xffffffffu : 0u;
 #pragma unroll
-        for (int m = 0; m < kQ; ++m) {
-            qb[m] = *reinterpret_cast<const uint4*>(qp + 32 * m);
-            if (!row_ok) qb[m] = make_uint4(0u, 0u, 0u, 0u);
-        }
-    }
+    for (int m = 0; m < kQ; ++m) qb[m] = make_uint4(qb[m].x & keep_q, qb[m].y & keep_q, qb[m].z & keep_q, qb[m].w & keep_q);
     const float scale2 = KV8 && p.k_scales ? p.scale2 * p.k_scales[job.g] : p.scale2;
-    const float slope2 = row_ok && p.slopes ? p.slopes[head] * kLog2e : 0.f;
+    const float slope2 = row_ok ? slope * kLog2e : 0.f;
     const float posf = (float)pos;
     f32x16 key_bias;                                             // slope * (key's offset in its tile) / score scale: the scores start from it
     {
@@ -223,11 +268,16 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
     bool started = !row_ok;
 
     const int k_at = Tile::row_at(n32, h2);
-    auto scores = [&](int at) __attribute__((always_inline)) {
+    // `between`: what is issued behind the reads of the first four operands (a step's loads to LDS)
+    auto scores = [&](int at, auto between) __attribute__((always_inline)) {
         f32x16 st = key_bias;
+        auto read = [&](int m) __attribute__((always_inline)) { return *reinterpret_cast<const uint4*>(lds + at + k_at + Tile::dims_at(m)); };
+        uint4 ka[4];
 #pragma unroll
-        for (int m = 0; m < kQ; ++m)
-            st = mfma32<DT>(*reinterpret_cast<const uint4*>(lds + at + k_at + Tile::dims_at(m)), qb[m], st);
+        for (int m = 0; m < 4; ++m) ka[m] = read(m);
+        between();
+#pragma unroll
+        for (int m = 0; m < kQ; ++m) st = mfma32<DT>(m < 4 ? ka[m & 3] : read(m), qb[m], st);
         return st;
     };
     uint32_t pk[2][4], pk_lo[2][4];                              // weights as pairs of 2-byte values (and what is left of them)
@@ -330,109 +380,108 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
         }
     };
     auto first_key = [&](int j) __attribute__((always_inline)) { return kbeg + kPfKeys * (j * KS + kw); };
-    auto weigh = [&](int j, f32x16 st) __attribute__((always_inline)) {
-        const int key0 = first_key(j);
-        if (key0 + kPfKeys > least) softmax(key0, st, std::true_type{});
-        else softmax(key0, st, std::false_type{});
-    };
-    auto add = [&](int j, int at) __attribute__((always_inline)) {
-        const int key0 = first_key(j);
-        if (key0 + kPfKeys > least) output_cut(key0, at);
-        else output(at);
+    auto finish = [&](int j, const f32x16& st, int at_v, auto masked) __attribute__((always_inline)) {
+        softmax(first_key(j), st, masked);
+        if (decltype(masked)::value) output_cut(first_key(j), at_v);
+        else output(at_v);
     };
     auto reads_done = [] __attribute__((always_inline)) () { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
 
     // ---- the walk -----------------------------------------------------------------------------------------
-    if constexpr (RW > 1) {
-        // a key group's tiles in a ring of NBUF buffers, asked for NBUF - 1 steps ahead; one barrier a step
-        constexpr int kLoads = 2 * kWaveGroups;                  // of a wave, per tile
+    // Steps [0, whole) of this wave's need no mask: loops of their own, whose bodies are straight lines.  (Waves of a workgroup may be in
+    // different loops: both have the same barriers.)
+    const int mine = (ntiles - kw + KS - 1) / KS;                // tiles of this wave's key group
+    const int whole = min(mine, max(0, (least - kbeg) / kPfKeys - kw + KS - 1) / KS);
+    if constexpr (RW > 1 && !KV8) {
+        auto step = [&](int j, const f32x16& st_cur, f32x16& st_ahead, auto masked) __attribute__((always_inline)) {
+            // K tile j + 1 and V tile j are there; newer: step j - 1's, where it asked for all of its own
+            if (kLead > 1 && j + kLead < mine) wait_direct<(kLead - 1) * kLoads>();
+            else wait_direct();
+            __syncthreads();                                     // ... for all; and the buffers read in step j - 1 are free
+            st_ahead = scores(buffer(j + 1), [&]() __attribute__((always_inline)) {
+                if (j + kLead < mine) {
+                    ask_k(j + 1 + kLead);
+                    ask_v(j + kLead);
+                }
+            });
+            if (!decltype(masked)::value || j < mine) finish(j, st_cur, buffer_v(j), masked);
+        };
+        f32x16 st, st_other;
+        if (mine > kLead) wait_direct<kLead * kLoads>();         // K tile 0 (newer: kLead K tiles, kLead V tiles)
+        else wait_direct();
+        __syncthreads();
+        st = scores(buffer(0), [] {});
+        int j = 0;
+        for (; j + 1 < whole; j += 2) {
+            step(j, st, st_other, std::false_type{});
+            step(j + 1, st_other, st, std::false_type{});
+        }
+        if (j < whole) {
+            step(j, st, st_other, std::false_type{});
+            st = st_other;
+            ++j;
+        }
+        for (; j < steps; ++j) {
+            step(j, st, st_other, std::true_type{});
+            st = st_other;
+        }
+    } else if constexpr (RW > 1) {
+        // 8-bit caches: codes wait in registers while the tile before is worked on
+        auto land = [&](int j) __attribute__((always_inline)) {
+            put(stage_k, buffer(j));
+            put(stage_v, buffer_v(j));
+        };
         auto bring = [&](int j) __attribute__((always_inline)) {
             const Runs runs = runs_of(j);
-            if constexpr (KV8) {
-                fetch(runs, kc, stage_k);
-                fetch(runs, vc, stage_v);
-            } else {
-                ask(runs, kc, buffer(j));
-                ask(runs, vc, buffer(j) + Tile::kTile);
-            }
+            fetch(runs, kc, stage_k);
+            fetch(runs, vc, stage_v);
         };
-        auto land = [&](int j) __attribute__((always_inline)) {  // 8-bit caches: what was fetched last
-            put(stage_k, buffer(j));
-            put(stage_v, buffer(j) + Tile::kTile);
+        if (has(0)) land(0);
+        if (has(1)) bring(1);
+        auto step = [&](int j, auto masked) __attribute__((always_inline)) {
+            __syncthreads();                                     // tile j is there for all, the buffers of tile j - 1 free
+            if (has(j + 1)) land(j + 1);
+            if (has(j + 2)) bring(j + 2);
+            if (!decltype(masked)::value || j < mine) finish(j, scores(buffer(j), [] {}), buffer_v(j), masked);
         };
-        if constexpr (KV8) {
-            if (has(0)) {
-                bring(0);
-                land(0);
-            }
-            if (has(1)) bring(1);
-        } else {
-#pragma unroll
-            for (int j = 0; j < NBUF - 1; ++j)
-                if (has(j)) bring(j);
-        }
-        for (int j = 0; j < steps; ++j) {
-            if constexpr (!KV8) {
-                if (NBUF > 2 && has(j + NBUF - 2)) wait_direct<(NBUF - 2) * kLoads>();
-                else wait_direct();
-            }
-            __syncthreads();                                     // tile j is there for all, the buffer of tile j - 1 free
-            if constexpr (KV8) {
-                if (has(j + 1)) land(j + 1);
-                if (has(j + 2)) bring(j + 2);
-            } else {
-                if (has(j + NBUF - 1)) bring(j + NBUF - 1);
-            }
-            if (has(j)) {
-                weigh(j, scores(buffer(j)));
-                add(j, buffer(j) + Tile::kTile);
-            }
-        }
+        int j = 0;
+        for (; j < whole; ++j) step(j, std::false_type{});
+        for (; j < steps; ++j) step(j, std::true_type{});
     } else {
-        // a wave's own tiles, one buffer: the next K tile is asked for when this one's scores are there, the next V
-        // tile when this one's output is
-        const int at_k = buffer(0), at_v = at_k + Tile::kTile;
-        Runs runs;
-        if (has(0)) {
-            runs = runs_of(0);
-            if constexpr (KV8) {
-                fetch(runs, kc, stage_k);
-                fetch(runs, vc, stage_v);
-            } else {
-                ask(runs, kc, at_k);
-                ask(runs, vc, at_v);
-            }
-        }
-        for (int j = 0; has(j); ++j) {
-            const bool more = has(j + 1);
+        auto step = [&](int j, auto masked) __attribute__((always_inline)) {
+            const bool more = j + 1 < mine;
             if constexpr (KV8) {
                 put(stage_k, at_k);
                 put(stage_v, at_v);
                 if (more) {
-                    runs = runs_of(j + 1);
+                    const Runs runs = runs_of(j + 1);
                     fetch(runs, kc, stage_k);
                     fetch(runs, vc, stage_v);
                 }
                 wave_lds_fence();
-                weigh(j, scores(at_k));
-                add(j, at_v);
+                finish(j, scores(at_k, [] {}), at_v, masked);
                 wave_lds_fence();
             } else {
                 wait_direct<kWaveGroups>();                      // (V tile j is newer)
-                const f32x16 st = scores(at_k);
+                const f32x16 st = scores(at_k, [] {});
                 reads_done();
+                Runs runs;
                 if (more) {
                     runs = runs_of(j + 1);
                     ask(runs, kc, at_k);
                 }
-                weigh(j, st);
+                softmax(first_key(j), st, masked);
                 if (more) wait_direct<kWaveGroups>();
                 else wait_direct();
-                add(j, at_v);
+                if (decltype(masked)::value) output_cut(first_key(j), at_v);
+                else output(at_v);
                 reads_done();
                 if (more) ask(runs, vc, at_v);
             }
-        }
+        };
+        int j = 0;
+        for (; j < whole; ++j) step(j, std::false_type{});
+        for (; j < mine; ++j) step(j, std::true_type{});
     }
 
     // ---- what it leaves: the key groups' results joined, one piece for each row block ---------------------------
@@ -489,6 +538,7 @@ __global__ __launch_bounds__(kCommonThreads, 2) void common_prefix_kernel(const 
 {
     CommonJob job;
     int row_waves;
+    const int lane = threadIdx.x & 63;
     if ((int)blockIdx.x < p.p_workgroups) {
         // workgroups go to XCD (number % 8): the row tiles of one (KV head, range of keys), which read the same tiles, to one
         const int x = blockIdx.x & 7, w = blockIdx.x >> 3, unit8 = p.by_p_tiles.div(w);
@@ -501,6 +551,8 @@ __global__ __launch_bounds__(kCommonThreads, 2) void common_prefix_kernel(const 
         job.table = p.prefix_table;
         job.kbeg = range * p.p_keys;
         job.kend = min(job.kbeg + p.p_keys, p.prefix_len);
+        job.held_first = job.kbeg >> p.block_shift;
+        job.held = job.table[min(job.held_first + lane, (p.prefix_len - 1) >> p.block_shift)];
         job.row0 = tile * 32 * row_waves;
         job.num_rows = p.rows;
         job.tok0 = job.pos0 = 0;
@@ -513,6 +565,11 @@ __global__ __launch_bounds__(kCommonThreads, 2) void common_prefix_kernel(const 
         row_waves = p.s_row_waves;
         job.prefix = false;
         job.g = unit - rest * p.num_kv_heads;
+        // (asked for together with the lengths: entries of the row beyond the sequence's blocks are not used)
+        job.table = p.block_tables + (int64_t)b * p.max_blocks_per_seq;
+        job.kbeg = p.prefix_len + range * p.s_keys;
+        job.held_first = job.kbeg >> p.block_shift;
+        job.held = job.table[min(job.held_first + lane, p.max_blocks_per_seq - 1)];
         const int cu0 = p.cu_q_lens ? p.cu_q_lens[b] : b, n_b = p.cu_q_lens ? p.cu_q_lens[b + 1] - cu0 : 1;
         job.row0 = tile * 32 * row_waves;
         job.num_rows = n_b * p.group;
@@ -521,11 +578,9 @@ __global__ __launch_bounds__(kCommonThreads, 2) void common_prefix_kernel(const 
         job.pos0 = p.context_lens[b] - n_b;
         // to the position of the tile's last row; the last range takes what there is
         const int last_row = min(job.row0 + 32 * row_waves, job.num_rows) - 1;
-        job.kbeg = p.prefix_len + range * p.s_keys;
         job.kend = job.pos0 + p.by_group.div(last_row) + 1;
         if (range + 1 < p.s_splits) job.kend = min(job.kend, job.kbeg + p.s_keys);
         if (job.kend <= job.kbeg) return;
-        job.table = p.block_tables + (int64_t)b * p.max_blocks_per_seq;
         job.slot = p.s_first + ((int64_t)range * p.num_kv_heads + job.g) * p.s_slots + (int)(((int64_t)cu0 * p.group) >> 5) + b + tile * row_waves;
     }
     if (row_waves == 4) common_body<DT, KV8, D, 4>(p, job);
@@ -544,42 +599,69 @@ __global__ __launch_bounds__(kCommonThreads) void common_join_kernel(const Commo
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int tile = p.by_kv_heads.div(blockIdx.x), g = blockIdx.x - tile * p.num_kv_heads, db = blockIdx.y;
     const int r = 32 * tile + n32, rc = min(r, p.rows - 1), t = p.by_group.div(rc), head = g * p.group + (rc - t * p.group);
-    const TokenPlace at = place_of_token(p, t);
-    // ranges in which the row sees a key
-    const int seen = at.pos + 1, in_prefix = min(seen, p.prefix_len), behind = seen - p.prefix_len;
-    const int np = in_prefix > 0 ? (in_prefix + p.p_keys - 1) / p.p_keys : 0;
-    const int ns = behind > 0 && p.s_splits > 0 ? min((behind + p.s_keys - 1) / p.s_keys, p.s_splits) : 0;
-    // own pieces: this row's place in the first
-    int64_t slot = 0;
-    int own_lane = 0;
-    if (ns > 0) {
-        const int64_t first_row = (int64_t)(p.cu_q_lens ? p.cu_q_lens[at.seq] : at.seq) * p.group;
-        const int in_seq = rc - (int)first_row;
-        slot = p.s_first + (int64_t)g * p.s_slots + (first_row >> 5) + at.seq + (in_seq >> 5);
-        own_lane = in_seq & 31;
-    }
-    const int most = wave_max(np + ns);
+    const PlaceGuess guess(p, t);
     float m = -INFINITY, l = 0.f;
     float4 acc[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = wave; i < most; i += kCommonWaves) {
-        if (i >= np + ns) continue;
-        int64_t s = ((int64_t)i * p.num_kv_heads + g) * p.p_slots + tile;
-        int sl = n32;
-        if (i >= np) s = slot + (int64_t)(i - np) * p.num_kv_heads * p.s_slots, sl = own_lane;
-        const float2 t2 = p.ml[s * 32 + sl];
-        const float4* const o = p.o + s * (kPieces * 64) + 4 * db * 64 + sl + 32 * h2;
-        const float m_new = fmaxf(m, t2.x);
-        const float f0 = m == -INFINITY ? 0.f : fast_exp2(m - m_new), f1 = t2.x == -INFINITY ? 0.f : fast_exp2(t2.x - m_new);
-        m = m_new;
-        l = fmaf(f1, t2.y, l * f0);
+    // kAtOnce pieces' loads in flight together.  at(i): piece i's number and the lane's row in it; i < n for the lane
+    constexpr int kAtOnce = 4;
+    auto join = [&](int n, int most, auto at) __attribute__((always_inline)) {
+        for (int i0 = wave; i0 < most; i0 += kCommonWaves * kAtOnce) {
+            float2 t2[kAtOnce];
+            float4 x[kAtOnce][4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float4 x = o[64 * j];
-            acc[j].x = fmaf(f1, x.x, acc[j].x * f0), acc[j].y = fmaf(f1, x.y, acc[j].y * f0);
-            acc[j].z = fmaf(f1, x.z, acc[j].z * f0), acc[j].w = fmaf(f1, x.w, acc[j].w * f0);
+            for (int k = 0; k < kAtOnce; ++k) {
+                const int i = i0 + kCommonWaves * k;
+                t2[k] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[k][j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (i < n) {
+                    int row;
+                    const int64_t piece = at(i, row);
+                    t2[k] = p.ml[piece * 32 + row];
+                    const float4* const o = p.o + piece * (kPieces * 64) + 4 * db * 64 + row + 32 * h2;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[k][j] = o[64 * j];
+                }
+            }
+            float m_new = m;
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) m_new = fmaxf(m_new, t2[k].x);
+            const float f0 = m == -INFINITY ? 0.f : fast_exp2(m - m_new);
+            m = m_new;
+            l *= f0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j].x *= f0, acc[j].y *= f0, acc[j].z *= f0, acc[j].w *= f0;
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                const float f = t2[k].x == -INFINITY ? 0.f : fast_exp2(t2[k].x - m);
+                l = fmaf(f, t2[k].y, l);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    acc[j].x = fmaf(f, x[k][j].x, acc[j].x), acc[j].y = fmaf(f, x[k][j].y, acc[j].y);
+                    acc[j].z = fmaf(f, x[k][j].z, acc[j].z), acc[j].w = fmaf(f, x[k][j].w, acc[j].w);
+                }
+            }
         }
+    };
+    // the prefix's pieces are there for every row, whatever it sees (m = -inf: nothing)
+    join(p.p_splits, p.p_splits, [&](int i, int& row) __attribute__((always_inline)) {
+        row = n32;
+        return ((int64_t)i * p.num_kv_heads + g) * p.p_slots + tile;
+    });
+    // its own: the ranges in which it sees a key
+    if (p.s_splits > 0) {
+        const TokenPlace at = guess.find(p, t);
+        const int seq = at.seq, behind = at.pos(t) + 1 - p.prefix_len;
+        const int n = behind > 0 ? min((behind + p.s_keys - 1) / p.s_keys, p.s_splits) : 0;
+        const int64_t first_row = (int64_t)(p.cu_q_lens && seq >= 0 ? p.cu_q_lens[seq] : max(seq, 0)) * p.group;
+        const int in_seq = rc - (int)first_row;
+        const int64_t slot = p.s_first + (int64_t)g * p.s_slots + (first_row >> 5) + seq + (in_seq >> 5);
+        join(n, wave_max(n), [&](int i, int& row) __attribute__((always_inline)) {
+            row = in_seq & 31;
+            return slot + (int64_t)i * p.num_kv_heads * p.s_slots;
+        });
     }
     xml[wave][lane] = make_float2(m, l);
 #pragma unroll

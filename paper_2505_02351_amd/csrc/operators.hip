@@ -186,13 +186,13 @@ CommonPlan plan_common(int64_t num_tokens, int64_t num_seqs, int num_heads, int 
     c.p_tiles = 1, c.p_keys = c.s_keys = 32, c.s_tiles = 1;
     if (prefix_len > 0) {
         c.p_tiles = (int)((c.p_slots + c.p_row_waves - 1) / c.p_row_waves);
-        common_ranges(prefix_len, (int64_t)num_kv_heads * c.p_tiles, 2 * num_cus(), prefix_len, c.p_row_waves, c.p_splits, c.p_keys);
+        common_ranges(prefix_len, (int64_t)num_kv_heads * c.p_tiles, num_cus(), prefix_len, c.p_row_waves, c.p_splits, c.p_keys);
     }
     const int64_t behind = max_context_len - prefix_len, own_rows = std::min(max_q_len, num_tokens) * group;
     c.s_row_waves = common_row_waves(own_rows);
     if (behind > 0) {
         c.s_tiles = (int)((own_rows + 32 * c.s_row_waves - 1) / (32 * c.s_row_waves));
-        common_ranges(behind, num_seqs * num_kv_heads * c.s_tiles, 2 * num_cus(), 1024, c.s_row_waves, c.s_splits, c.s_keys);
+        common_ranges(behind, num_seqs * num_kv_heads * c.s_tiles, num_cus(), 2048, c.s_row_waves, c.s_splits, c.s_keys);
     }
     c.p_units = (int64_t)num_kv_heads * c.p_splits;
     c.s_units = num_seqs * num_kv_heads * c.s_splits;

@@ -173,6 +173,13 @@ def test_lengths_at_their_ends(G, bounds, D):
         batch.check(batch.run(G, bounds=bounds))
 
 
+@pytest.mark.parametrize("new", [[4, 1], [3, 0, 1], [1, 1, 2, 1], [0, 1], [1, 0], [1, 1, 0, 1, 1]])
+def test_last_sequence_with_one_new_token(G, new):
+    """Prefix sums that look like one new token each in places."""
+    batch = Batch(12, "f16", 8, 2, 64, 16, 3, [48 + 20 + 7 * i for i in range(len(new))], new).upload()
+    batch.check(batch.run(G))
+
+
 def test_a_context_shorter_than_its_new_tokens(G):
     """Positions below 0 see nothing."""
     batch = Batch(4, "f16", 8, 2, 64, 16, 2, [3, 40], [5, 2]).upload()
