@@ -6,7 +6,9 @@
 // Here the cuts are
 //   the prefix     the rows of ALL sequences - every new token, every head of the group - against its keys, cut into ranges of
 //                  p_keys: a dense contraction whose K and V tiles serve up to 128 rows at a time;
-//   own parts      the rows of ONE sequence against the keys behind the prefix, cut into ranges of s_keys.
+//   own parts      the rows of ONE sequence against the keys behind the prefix.  Lengths are ragged and known on the device only: the
+//                  steps (of 128, 64 or 32 keys) of all (sequence, KV head, row tile) segments, divided by a number of shares, are
+//                  the longest that a piece may be, and each segment is cut into so many equal pieces.
 // One launch computes all pieces (a workgroup each), a second joins them.  A row sees keys 0 .. its position, wherever the
 // prefix ends.
 //
@@ -41,13 +43,13 @@ struct CommonParams {
     int prefix_len;             // keys
     int rows;                   // num_tokens * group: of a KV head
     int p_row_waves, p_tiles, p_splits, p_keys, p_units, p_workgroups;      // tiles: workgroups' row tiles; units: KV head, range
-    int s_row_waves, s_tiles, s_splits, s_keys, s_units;                    // units: sequence, KV head, range
-    // pieces, 32 rows each: of the prefix [range][KV head][p_slots], then own ones [range][KV head][s_slots]
-    int p_slots, s_slots;
+    int s_row_waves, s_shares;
+    // pieces, 32 rows each: of the prefix [range][KV head][p_slots]; then s_row_waves for each own one
+    int p_slots;
     int64_t s_first;
     float4* o;                  // per piece [D / 8][64]: what lane l of the wave holds, dims 8i + 4 (l / 32) .. + 3 of row l % 32
     float2* ml;                 // per piece [32]: m, l
-    FastDiv by_group, by_p_tiles, by_s_tiles, by_kv_heads, by_seqs;
+    FastDiv by_group, by_p_tiles, by_kv_heads, by_s_shares;
 };
 
 template <int D> constexpr int kCommonLds = [] {
@@ -55,11 +57,11 @@ template <int D> constexpr int kCommonLds = [] {
     return tiles > join ? tiles : join;
 }();
 
-// The sequence of token t (seq < 0: none has it), its context length and the token behind its last.  All lanes of a wave
+// The sequence of token t (seq < 0: none has it), its context length, its first token and the one behind its last.  All lanes of a wave
 // together: first the guess that every sequence has one new token, which one round trip to memory confirms, else the sequences'
 // ends and lengths, 64 at a time, one a lane.
 struct TokenPlace {
-    int seq, len, end;
+    int seq, len, first, end;
     __device__ __forceinline__ int pos(int t) const { return seq < 0 ? -1 : len - end + t; }
 };
 // What the guess needs, asked for here and used by find() (so that other loads can be asked for in between).
@@ -74,12 +76,12 @@ struct PlaceGuess {
     }
     __device__ __forceinline__ TokenPlace find(const CommonParams& p, int t) const
     {
-        if (__builtin_amdgcn_ballot_w64(first != t || end != t + 1) == 0) return {seq, len, end};
+        if (__builtin_amdgcn_ballot_w64(first != t || end != t + 1) == 0) return {seq, len, first, end};
         const int lane = threadIdx.x & 63;
-        TokenPlace at{-1, 0, 0};
+        TokenPlace at{-1, 0, 0, 0};
         for (int from = 0; from < p.num_seqs; from += 64) {
             const int n = min(p.num_seqs - from, 64), b = from + min(lane, n - 1);
-            const int ends = p.cu_q_lens[b + 1], lens = p.context_lens[b];
+            const int starts = p.cu_q_lens[b], ends = p.cu_q_lens[b + 1], lens = p.context_lens[b];
             int k = 0;                                           // of the n sequences, those that end at or before t
 #pragma unroll
             for (int s = 32; s; s >>= 1) {
@@ -88,12 +90,64 @@ struct PlaceGuess {
             }
             const int next = __shfl(ends, k & 63);
             if (k + 1 <= n && next <= t) ++k;
-            const int e = __shfl(ends, k & 63), l = __shfl(lens, k & 63);
-            if (at.seq < 0 && k < n) at = {from + k, l, e};
+            const int first_k = __shfl(starts, k & 63), len_k = __shfl(lens, k & 63);
+            if (at.seq < 0 && k < n) at = {from + k, len_k, first_k, next};
         }
         return at;
     }
 };
+
+// inclusive sum over the lanes
+__device__ __forceinline__ int lane_sums(int x)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int y = __shfl_up(x, off);
+        x += lane >= off ? y : 0;
+    }
+    return x;
+}
+
+// Own parts of 64 sequences, one a lane.  A segment: one KV head, one row tile.
+struct OwnParts {
+    int len, first, rows;       // context length, first token, rows (new tokens x heads of the group)
+    int steps, segments;        // of a segment; segments (0: nothing to do)
+    int pieces, before;         // of a segment; pieces of all sequences before this one (number())
+    static __device__ __forceinline__ int keys_shift(const CommonParams& p) { return 7 - (p.s_row_waves >> 1); }       // a step's: 128, 64, 32 for 1, 2, 4
+    static __device__ __forceinline__ int steps_of(const CommonParams& p, int keys) { return (keys + (1 << keys_shift(p)) - 1) >> keys_shift(p); }
+    // those from number `from` on
+    __device__ __forceinline__ OwnParts(const CommonParams& p, int from)
+    {
+        const int lane = threadIdx.x & 63, b = min(from + lane, p.num_seqs - 1);
+        len = p.context_lens[b];
+        first = p.cu_q_lens ? p.cu_q_lens[b] : b;
+        rows = (p.cu_q_lens ? p.cu_q_lens[b + 1] - first : 1) * p.group;
+        const int behind = from + lane < p.num_seqs && rows > 0 ? max(len - p.prefix_len, 0) : 0;
+        steps = steps_of(p, behind);
+        segments = behind > 0 ? ((rows + 32 * p.s_row_waves - 1) >> (4 + 32 - __builtin_clz(p.s_row_waves))) * p.num_kv_heads : 0;
+    }
+    // a segment has as many equal pieces as shares of `most` steps take; `all`: pieces before these sequences, and then with them
+    __device__ __forceinline__ void number(int most, int& all)
+    {
+        pieces = div_by_inverse(steps + most - 1, most, __builtin_amdgcn_rcpf((float)most));
+        const int mine = pieces * segments, sum = lane_sums(mine);
+        before = all + sum - mine;
+        all += __builtin_amdgcn_readlane(sum, 63);
+    }
+    // steps of a piece
+    static __device__ __forceinline__ int each(int steps, int pieces) { return div_by_inverse(steps + pieces - 1, pieces, __builtin_amdgcn_rcpf((float)pieces)); }
+};
+// The most steps of a piece.  `parts`: the first 64 sequences'.
+__device__ __forceinline__ int own_share(const CommonParams& p, const OwnParts& parts)
+{
+    int total = wave_sum(parts.steps * parts.segments);
+    for (int from = 64; from < p.num_seqs; from += 64) {
+        const OwnParts more(p, from);
+        total += wave_sum(more.steps * more.segments);
+    }
+    return max(p.by_s_shares.div(total + p.s_shares - 1), 1);
+}
 
 // A workgroup's rows and keys.
 struct CommonJob {
@@ -205,8 +259,11 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
     // 2-byte caches: straight to LDS
     auto ask = [&](const Runs& r, const unsigned char* cache, int at) __attribute__((always_inline)) {
 #pragma unroll
-        for (int n = 0; n < kWaveGroups; ++n)
-            load_direct(lds0 + at + (rw * kWaveGroups + n) * Tile::kGroup, cache + r.at[n / kRunGroups], r.lane_at[n]);
+        for (int n = 0; n < kWaveGroups; ++n) {
+            const uint32_t to = lds0 + at + (rw * kWaveGroups + n) * Tile::kGroup;
+            if (RW == 1) stream_direct(to, cache + r.at[n / kRunGroups], r.lane_at[n]);      // (no other row tile reads them)
+            else load_direct(to, cache + r.at[n / kRunGroups], r.lane_at[n]);
+        }
     };
     // 8-bit caches: codes to registers, widened on the way into LDS
     u32x2 stage_k[KV8 ? kWaveGroups : 1], stage_v[KV8 ? kWaveGroups : 1];
@@ -487,7 +544,6 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
     // ---- what it leaves: the key groups' results joined, one piece for each row block ---------------------------
     const float l_row = lsum + __shfl_xor(lsum, 32);
     const float m_row = started && row_ok ? m_ref : -INFINITY;
-    const bool exists = job.row0 + 32 * rw < job.num_rows;       // wave-uniform
     float4* const o = p.o + (job.slot + rw) * (kPieces * 64) + lane;
     float2* const ml = p.ml + (job.slot + rw) * 32 + n32;
     auto piece_of = [&](int i) __attribute__((always_inline)) {
@@ -496,10 +552,11 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
         return make_float4(a[e], a[e + 1], a[e + 2], a[e + 3]);
     };
     if constexpr (KS == 1) {
-        if (!exists) return;
+        if (row_ok) {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) o[64 * i] = piece_of(i);
-        if (h2 == 0) *ml = make_float2(m_row, l_row);
+            for (int i = 0; i < kPieces; ++i) o[64 * i] = piece_of(i);
+            if (h2 == 0) *ml = make_float2(m_row, l_row);
+        }
     } else {
         float4* const xo = reinterpret_cast<float4*>(lds);       // [wave][piece][lane]
         float2* const xml = reinterpret_cast<float2*>(lds + kCommonWaves * 64 * kPieces * 16);
@@ -508,7 +565,6 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
         for (int i = 0; i < kPieces; ++i) xo[(wave * kPieces + i) * 64 + lane] = piece_of(i);
         xml[wave * 64 + lane] = make_float2(m_row, l_row);
         __syncthreads();
-        if (!exists) return;
         float m_all = -INFINITY, f[KS], l_all = 0.f;
 #pragma unroll
         for (int k = 0; k < KS; ++k) m_all = fmaxf(m_all, xml[(k * RW + rw) * 64 + lane].x);
@@ -527,62 +583,66 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
                 const float4 x = xo[((k * RW + rw) * kPieces + piece) * 64 + lane];
                 s.x = fmaf(f[k], x.x, s.x), s.y = fmaf(f[k], x.y, s.y), s.z = fmaf(f[k], x.z, s.z), s.w = fmaf(f[k], x.w, s.w);
             }
-            o[64 * piece] = s;
+            if (row_ok) o[64 * piece] = s;
         }
-        if (kw == 0 && h2 == 0) *ml = make_float2(m_all, l_all);
+        if (kw == 0 && h2 == 0 && row_ok) *ml = make_float2(m_all, l_all);
     }
 }
 
 template <int DT, bool KV8, int D>
 __global__ __launch_bounds__(kCommonThreads, 2) void common_prefix_kernel(const CommonParams p)
 {
-    CommonJob job;
-    int row_waves;
     const int lane = threadIdx.x & 63;
-    if ((int)blockIdx.x < p.p_workgroups) {
+    CommonJob job;
+    job.prefix = (int)blockIdx.x < p.p_workgroups;
+    const int row_waves = job.prefix ? p.p_row_waves : p.s_row_waves;
+    if (job.prefix) {
         // workgroups go to XCD (number % 8): the row tiles of one (KV head, range of keys), which read the same tiles, to one
         const int x = blockIdx.x & 7, w = blockIdx.x >> 3, unit8 = p.by_p_tiles.div(w);
         const int unit = unit8 * 8 + x, tile = w - unit8 * p.p_tiles;
         if (unit >= p.p_units) return;
         const int range = p.by_kv_heads.div(unit);
-        row_waves = p.p_row_waves;
-        job.prefix = true;
         job.g = unit - range * p.num_kv_heads;
         job.table = p.prefix_table;
         job.kbeg = range * p.p_keys;
         job.kend = min(job.kbeg + p.p_keys, p.prefix_len);
-        job.held_first = job.kbeg >> p.block_shift;
-        job.held = job.table[min(job.held_first + lane, (p.prefix_len - 1) >> p.block_shift)];
         job.row0 = tile * 32 * row_waves;
         job.num_rows = p.rows;
         job.tok0 = job.pos0 = 0;
         job.slot = ((int64_t)range * p.num_kv_heads + job.g) * p.p_slots + tile * row_waves;
     } else {
-        const int i = blockIdx.x - p.p_workgroups, x = i & 7, w = i >> 3, unit8 = p.by_s_tiles.div(w);
-        const int unit = unit8 * 8 + x, tile = w - unit8 * p.s_tiles;
-        if (unit >= p.s_units) return;
-        const int rest = p.by_kv_heads.div(unit), range = p.by_seqs.div(rest), b = rest - range * p.num_seqs;
-        row_waves = p.s_row_waves;
-        job.prefix = false;
-        job.g = unit - rest * p.num_kv_heads;
-        // (asked for together with the lengths: entries of the row beyond the sequence's blocks are not used)
+        const int me = blockIdx.x - p.p_workgroups;              // the piece
+        OwnParts parts(p, 0);
+        const int share = own_share(p, parts);
+        int all = 0, from = 0;
+        parts.number(share, all);
+        while (all <= me) {                                      // not one of these sequences'
+            from += 64;
+            if (from >= p.num_seqs) return;                      // (nobody's)
+            parts = OwnParts(p, from);
+            parts.number(share, all);
+        }
+        const int l = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(parts.segments > 0 && parts.before <= me));
+        const int b = from + l, len = __builtin_amdgcn_readlane(parts.len, l), steps = __builtin_amdgcn_readlane(parts.steps, l);
+        const int pieces = __builtin_amdgcn_readlane(parts.pieces, l), in_seq = me - __builtin_amdgcn_readlane(parts.before, l);
+        const int segment = __builtin_amdgcn_readfirstlane(in_seq / pieces), each = __builtin_amdgcn_readfirstlane(OwnParts::each(steps, pieces));
+        const int lo = (in_seq - segment * pieces) * each, hi = min(lo + each, steps);
+        if (hi <= lo) return;                                    // (equal pieces of, say, 7 steps in 4: the last is empty)
+        job.num_rows = __builtin_amdgcn_readlane(parts.rows, l);
+        job.tok0 = __builtin_amdgcn_readlane(parts.first, l);
+        const int tiles = (job.num_rows + 32 * row_waves - 1) / (32 * row_waves);
+        job.g = __builtin_amdgcn_readfirstlane(segment / tiles);
+        job.row0 = (segment - job.g * tiles) * 32 * row_waves;
+        job.pos0 = len - p.by_group.div(job.num_rows);
+        // to the position of the tile's last row
+        job.kbeg = p.prefix_len + (lo << OwnParts::keys_shift(p));
+        job.kend = min(job.pos0 + p.by_group.div(min(job.row0 + 32 * row_waves, job.num_rows) - 1) + 1, p.prefix_len + (hi << OwnParts::keys_shift(p)));
+        if (job.kend <= job.kbeg) return;                        // (beyond what its rows see; the join knows)
         job.table = p.block_tables + (int64_t)b * p.max_blocks_per_seq;
-        job.kbeg = p.prefix_len + range * p.s_keys;
-        job.held_first = job.kbeg >> p.block_shift;
-        job.held = job.table[min(job.held_first + lane, p.max_blocks_per_seq - 1)];
-        const int cu0 = p.cu_q_lens ? p.cu_q_lens[b] : b, n_b = p.cu_q_lens ? p.cu_q_lens[b + 1] - cu0 : 1;
-        job.row0 = tile * 32 * row_waves;
-        job.num_rows = n_b * p.group;
-        if (job.row0 >= job.num_rows) return;
-        job.tok0 = cu0;
-        job.pos0 = p.context_lens[b] - n_b;
-        // to the position of the tile's last row; the last range takes what there is
-        const int last_row = min(job.row0 + 32 * row_waves, job.num_rows) - 1;
-        job.kend = job.pos0 + p.by_group.div(last_row) + 1;
-        if (range + 1 < p.s_splits) job.kend = min(job.kend, job.kbeg + p.s_keys);
-        if (job.kend <= job.kbeg) return;
-        job.slot = p.s_first + ((int64_t)range * p.num_kv_heads + job.g) * p.s_slots + (int)(((int64_t)cu0 * p.group) >> 5) + b + tile * row_waves;
+        job.slot = p.s_first + (int64_t)me * row_waves;
     }
+    job.held_first = job.kbeg >> p.block_shift;
+    job.held = job.table[min(job.held_first + lane, (job.kend - 1) >> p.block_shift)];
     if (row_waves == 4) common_body<DT, KV8, D, 4>(p, job);
     else if (row_waves == 2) common_body<DT, KV8, D, 2>(p, job);
     else common_body<DT, KV8, D, 1>(p, job);
@@ -650,17 +710,33 @@ __global__ __launch_bounds__(kCommonThreads) void common_join_kernel(const Commo
         row = n32;
         return ((int64_t)i * p.num_kv_heads + g) * p.p_slots + tile;
     });
-    // its own: the ranges in which it sees a key
-    if (p.s_splits > 0) {
+    // its own: the steps in which it sees a key, and the workgroups that had them
+    if (p.s_shares > 0) {
         const TokenPlace at = guess.find(p, t);
-        const int seq = at.seq, behind = at.pos(t) + 1 - p.prefix_len;
-        const int n = behind > 0 ? min((behind + p.s_keys - 1) / p.s_keys, p.s_splits) : 0;
-        const int64_t first_row = (int64_t)(p.cu_q_lens && seq >= 0 ? p.cu_q_lens[seq] : max(seq, 0)) * p.group;
-        const int in_seq = rc - (int)first_row;
-        const int64_t slot = p.s_first + (int64_t)g * p.s_slots + (first_row >> 5) + seq + (in_seq >> 5);
+        const int behind = at.pos(t) + 1 - p.prefix_len;
+        OwnParts parts(p, 0);
+        const int share = own_share(p, parts);
+        int n = 0, row_in_tile = 0, all = 0;
+        int64_t piece0 = 0;
+        for (int from = 0;;) {
+            parts.number(share, all);
+            const int l = at.seq - from;                         // (all lanes exchange)
+            const int before = __shfl(parts.before, l & 63), pieces = __shfl(parts.pieces, l & 63), steps = __shfl(parts.steps, l & 63);
+            if (behind > 0 && l >= 0 && l < 64) {
+                const int in_seq = rc - at.first * p.group, tile_rows = 32 * p.s_row_waves, tile_shift = 31 - __builtin_clz(tile_rows);
+                const int tiles = ((at.end - at.first) * p.group + tile_rows - 1) >> tile_shift;
+                const int each = OwnParts::each(steps, pieces);
+                n = div_by_inverse(OwnParts::steps_of(p, behind) + each - 1, each, __builtin_amdgcn_rcpf((float)each));
+                row_in_tile = in_seq & 31;
+                piece0 = p.s_first + (int64_t)(before + (g * tiles + (in_seq >> tile_shift)) * pieces) * p.s_row_waves + ((in_seq >> 5) & (p.s_row_waves - 1));
+            }
+            from += 64;
+            if (from >= p.num_seqs) break;
+            parts = OwnParts(p, from);
+        }
         join(n, wave_max(n), [&](int i, int& row) __attribute__((always_inline)) {
-            row = in_seq & 31;
-            return slot + (int64_t)i * p.num_kv_heads * p.s_slots;
+            row = row_in_tile;
+            return piece0 + (int64_t)i * p.s_row_waves;
         });
     }
     xml[wave][lane] = make_float2(m, l);

@@ -84,6 +84,11 @@ __device__ __forceinline__ void load_direct(uint32_t lds, const unsigned char* l
 {
     asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "{m0}"(lds), "v"(lane_addr) : "memory");
 }
+// (non-temporal: what is read once, see stream_load16)
+__device__ __forceinline__ void stream_direct(uint32_t lds, const unsigned char* base, uint32_t lane_off)
+{
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" :: "{m0}"(lds), "v"(lane_off), "s"(base) : "memory");
+}
 template <int NEWER = 0> __device__ __forceinline__ void wait_direct() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NEWER) : "memory"); }
 
 template <int DT> __device__ __forceinline__ uint32_t pack2(float lo, float hi) { return narrow2<DT>(lo, hi); }

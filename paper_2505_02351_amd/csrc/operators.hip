@@ -154,53 +154,53 @@ int launch_verify(const VerifyParams& a, int num_seqs, hipStream_t st)
 
 // How a common-prefix call is cut into pieces; the same for its workspace and its launch.
 struct CommonPlan {
-    int p_row_waves, p_tiles, p_splits, p_keys;
-    int s_row_waves, s_tiles, s_splits, s_keys;
-    int64_t rows, p_slots, s_slots, pieces, p_units, s_units;
-    int64_t workgroups() const { return (p_units + 7) / 8 * 8 * p_tiles + (s_units + 7) / 8 * 8 * s_tiles; }
-    bool fits() const { return rows < (1ll << 31) && workgroups() < (1ll << 31) && p_slots * 4 < (1ll << 31); }
+    int p_row_waves, p_tiles, p_splits, p_keys, s_row_waves, s_shares;
+    int64_t rows, p_slots, p_units, s_workgroups;                // s_workgroups: own pieces at most
+    int64_t p_pieces(int num_kv_heads) const { return num_kv_heads * p_splits * p_slots; }
+    int64_t workgroups() const { return (p_units + 7) / 8 * 8 * p_tiles + s_workgroups; }
+    int64_t pieces(int num_kv_heads) const { return p_pieces(num_kv_heads) + s_workgroups * s_row_waves; }
+    size_t bytes(int num_kv_heads, int head_dim) const { return (size_t)pieces(num_kv_heads) * 32 * (head_dim * sizeof(float) + sizeof(float2)); }
 };
 
 // Row blocks of a workgroup for so many rows: 1, 2 or 4 of 32.
 int common_row_waves(int64_t rows) { return rows > 64 ? 4 : rows > 32 ? 2 : 1; }
 
-// Ranges of `keys` keys: enough for `wanted` workgroups of `units`, none shorter than two tiles of 32 for each key group of the workgroup.
-void common_ranges(int64_t keys, int64_t units, int64_t wanted, int64_t at_most, int row_waves, int& splits, int& range)
+// false: sizes beyond the kernels' 32-bit counts
+bool plan_common(CommonPlan& c, int64_t num_tokens, int64_t num_seqs, int num_heads, int num_kv_heads, int64_t prefix_len, int64_t max_context_len,
+                 int64_t max_q_len)
 {
-    const int64_t step = 32 * (kCommonWaves / row_waves);
-    int64_t n = std::max<int64_t>(std::min<int64_t>(wanted / std::max<int64_t>(units, 1), keys / (2 * step)), (keys + at_most - 1) / at_most);
-    n = std::max<int64_t>(n, 1);
-    const int64_t each = ((keys + n - 1) / n + step - 1) / step * step;
-    range = (int)each;
-    splits = (int)((keys + each - 1) / each);
-}
-
-CommonPlan plan_common(int64_t num_tokens, int64_t num_seqs, int num_heads, int num_kv_heads, int64_t prefix_len, int64_t max_context_len, int64_t max_q_len)
-{
-    const int64_t group = num_heads / num_kv_heads;
-    CommonPlan c{};
+    const int64_t group = num_heads / num_kv_heads, cus = num_cus();
+    c = CommonPlan{};
     c.rows = num_tokens * group;
     c.p_slots = (c.rows + 31) / 32;
-    c.s_slots = c.rows / 32 + num_seqs;                          // a sequence's first: its first row / 32 + its number
     c.p_row_waves = common_row_waves(c.rows);
-    c.p_tiles = 1, c.p_keys = c.s_keys = 32, c.s_tiles = 1;
+    c.p_tiles = 1, c.p_keys = 32;
+    if (c.rows >= (1ll << 31) - 64 || c.p_slots * num_kv_heads >= (1ll << 31)) return false;
+    // A workgroup of each kind to a CU: the prefix's is bound by its matrix and vector instructions, the own parts' by memory.
     if (prefix_len > 0) {
         c.p_tiles = (int)((c.p_slots + c.p_row_waves - 1) / c.p_row_waves);
-        common_ranges(prefix_len, (int64_t)num_kv_heads * c.p_tiles, num_cus(), prefix_len, c.p_row_waves, c.p_splits, c.p_keys);
+        // ranges: none shorter than two tiles of 32 for each key group of a workgroup
+        const int64_t step = 32 * (kCommonWaves / c.p_row_waves), units = (int64_t)num_kv_heads * c.p_tiles;
+        const int64_t n = std::max<int64_t>(std::min(cus / units, prefix_len / (2 * step)), 1);
+        const int64_t each = ((prefix_len + n - 1) / n + step - 1) / step * step;
+        c.p_keys = (int)each;
+        c.p_splits = (int)((prefix_len + each - 1) / each);
+        c.p_units = (int64_t)num_kv_heads * c.p_splits;
     }
     const int64_t behind = max_context_len - prefix_len, own_rows = std::min(max_q_len, num_tokens) * group;
     c.s_row_waves = common_row_waves(own_rows);
     if (behind > 0) {
-        c.s_tiles = (int)((own_rows + 32 * c.s_row_waves - 1) / (32 * c.s_row_waves));
-        common_ranges(behind, num_seqs * num_kv_heads * c.s_tiles, num_cus(), 2048, c.s_row_waves, c.s_splits, c.s_keys);
+        const int64_t tile_rows = 32 * c.s_row_waves, step = 32 * (kCommonWaves / c.s_row_waves);
+        const int64_t steps = num_seqs * num_kv_heads * ((own_rows + tile_rows - 1) / tile_rows) * ((behind + step - 1) / step);
+        if (steps >= (1ll << 30)) return false;
+        // (a piece of half of all CUs' share: with more pieces, and with fewer, 64 sequences behind 4 096 tokens, own parts of 127 - 1 023, take
+        // 37 - 38 us instead of 32, behind 32 768, 1 023 - 2 047, 110 - 125 instead of 110)
+        c.s_shares = (int)std::min<int64_t>(std::max<int64_t>(cus / 2, 1), steps);
+        // no more than the shares and one for each segment
+        c.s_workgroups = c.s_shares + num_kv_heads * (c.rows / tile_rows + num_seqs);
     }
-    c.p_units = (int64_t)num_kv_heads * c.p_splits;
-    c.s_units = num_seqs * num_kv_heads * c.s_splits;
-    c.pieces = num_kv_heads * (c.p_splits * c.p_slots + c.s_splits * c.s_slots);
-    return c;
+    return c.workgroups() < (1ll << 31);
 }
-
-size_t common_bytes(const CommonPlan& c, int head_dim) { return (size_t)c.pieces * 32 * (head_dim * sizeof(float) + sizeof(float2)); }
 
 template <int DT, bool KV8, int D>
 int launch_common(const CommonParams& p, int workgroups, hipStream_t st)
@@ -243,9 +243,9 @@ int common_impl(void* out, const void* q, const void* k_cache, const void* v_cac
     if (!out || !q || !k_cache || !v_cache || !context_lens || (num_prefix_blocks && !prefix_table) || (max_context_len > prefix_len && !block_tables))
         return OPTGQA_ERR_NULL;
     if (!aligned16(out) || !aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache)) return OPTGQA_ERR_UNSUPPORTED;
-    const CommonPlan c = plan_common(num_tokens, num_seqs, num_heads, num_kv_heads, prefix_len, max_context_len, cu_q_lens ? max_q_len : 1);
-    if (!c.fits()) return OPTGQA_ERR_SHAPE;
-    if (!workspace || !aligned16(workspace) || workspace_bytes < common_bytes(c, head_dim)) return OPTGQA_ERR_WORKSPACE;
+    CommonPlan c;
+    if (!plan_common(c, num_tokens, num_seqs, num_heads, num_kv_heads, prefix_len, max_context_len, cu_q_lens ? max_q_len : 1)) return OPTGQA_ERR_SHAPE;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < c.bytes(num_kv_heads, head_dim)) return OPTGQA_ERR_WORKSPACE;
 
     CommonParams p;
     p.out = out;
@@ -283,20 +283,16 @@ int common_impl(void* out, const void* q, const void* k_cache, const void* v_cac
     p.p_units = (int)c.p_units;
     p.p_workgroups = (int)((c.p_units + 7) / 8 * 8 * c.p_tiles);
     p.s_row_waves = c.s_row_waves;
-    p.s_tiles = c.s_tiles;
-    p.s_splits = c.s_splits;
-    p.s_keys = c.s_keys;
-    p.s_units = (int)c.s_units;
+    p.s_shares = c.s_shares;
     p.p_slots = (int)c.p_slots;
-    p.s_slots = (int)c.s_slots;
-    p.s_first = c.p_splits * num_kv_heads * c.p_slots;
+    p.s_first = c.p_pieces(num_kv_heads);
+    const size_t pieces = (size_t)c.pieces(num_kv_heads);
     p.o = static_cast<float4*>(workspace);
-    p.ml = reinterpret_cast<float2*>(static_cast<unsigned char*>(workspace) + (size_t)c.pieces * 32 * head_dim * sizeof(float));
+    p.ml = reinterpret_cast<float2*>(static_cast<unsigned char*>(workspace) + pieces * 32 * head_dim * sizeof(float));
     p.by_group.set((uint32_t)p.group);
     p.by_p_tiles.set((uint32_t)c.p_tiles);
-    p.by_s_tiles.set((uint32_t)c.s_tiles);
     p.by_kv_heads.set((uint32_t)num_kv_heads);
-    p.by_seqs.set((uint32_t)num_seqs);
+    p.by_s_shares.set((uint32_t)std::max(c.s_shares, 1));
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int workgroups = (int)c.workgroups();
     if (dtype == OPTGQA_F16)
@@ -449,10 +445,14 @@ size_t optgqa_common_prefix_workspace_bytes(int num_tokens, int num_seqs, int nu
     if (num_tokens <= 0 || num_seqs <= 0 || num_heads <= 0 || num_kv_heads <= 0 || num_heads % num_kv_heads || !head_dim_ok(head_dim) ||
         !block_size_ok(block_size) || num_prefix_blocks < 0 || max_context_len < 0 || max_q_len <= 0)
         return 0;
-    const CommonPlan c = plan_common(num_tokens, num_seqs, num_heads, num_kv_heads, (int64_t)num_prefix_blocks * block_size, max_context_len, max_q_len);
     // (without prefix sums of new tokens a sequence has one, whatever the bound: the call needs the larger of the two)
-    const CommonPlan one = plan_common(num_tokens, num_seqs, num_heads, num_kv_heads, (int64_t)num_prefix_blocks * block_size, max_context_len, 1);
-    return std::max<size_t>(std::max(common_bytes(c, head_dim), common_bytes(one, head_dim)), 16);
+    size_t bytes = 16;
+    for (const int n : {max_q_len, 1}) {
+        CommonPlan c;
+        if (!plan_common(c, num_tokens, num_seqs, num_heads, num_kv_heads, (int64_t)num_prefix_blocks * block_size, max_context_len, n)) return 0;
+        bytes = std::max(bytes, c.bytes(num_kv_heads, head_dim));
+    }
+    return bytes;
 }
 
 int optgqa_paged_attention_common(void* out, const void* q, const void* k_cache, const void* v_cache, const int32_t* prefix_table,
