@@ -52,23 +52,56 @@ def rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: int = RO
     return freqs, magnitude.value
 
 
-def _rows(t: torch.Tensor, name: str, tokens: int) -> Tuple[int, int]:
+# The checks below run on every call, and a call for one token is bound by them: a tensor costs 0.2 us here.
+def _refuse(t, name: str, dtype: torch.dtype, index: int) -> None:
+    """Why _check_tensors does not take a tensor: its type first, then its place."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"optgqa: {name} must be a torch.Tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"optgqa: {name} must be {dtype}, got {t.dtype}")
+    if index < 0:
+        raise ValueError("optgqa: tensors must live in GPU memory")
+    raise ValueError(f"optgqa: {name} is on {t.device}, expected GPU {index}")
+
+
+def _check_tensors(index: int, tensors) -> None:
+    """(tensor, name, type) each: element type, and GPU `index`.  Types before places, as everywhere in the package."""
+    wrong = None
+    for x in tensors:
+        t = x[0]
+        if type(t) is not torch.Tensor and not isinstance(t, torch.Tensor) or t.dtype is not x[2]:
+            _refuse(*x, index)
+        if t.get_device() != index or index < 0:
+            wrong = wrong or x
+    if wrong:
+        _refuse(*wrong, index)
+
+
+def _dense(*tensors) -> None:
+    for t, name in tensors:
+        if not t.is_contiguous():
+            raise ValueError(f"optgqa: {name} must be contiguous")
+
+
+def _rows(t: torch.Tensor, name: str, tokens: int, D: int) -> Tuple[int, int]:
     """(heads, token stride) of a [T, heads, D] tensor whose tokens' rows are dense."""
-    if t.dim() != 3 or t.shape[0] != tokens:
-        raise ValueError(f"optgqa: {name} must be [{tokens}, heads, head_dim], got {tuple(t.shape)}")
-    T, H, D = t.shape
-    if T and H and (t.stride(2) != 1 or (H > 1 and t.stride(1) != D)):
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != tokens or shape[2] != D:
+        raise ValueError(f"optgqa: {name} must be [{tokens}, heads, {D}], got {tuple(shape)}")
+    H, stride = shape[1], t.stride()
+    if tokens > 1 and H and (stride[2] != 1 or (H > 1 and stride[1] != D)) or tokens == 1 and H > 1 and (stride[2] != 1 or stride[1] != D):
         raise ValueError(f"optgqa: {name} must be dense in its last two dims")
-    return H, t.stride(0) if T > 1 else H * D
+    return H, stride[0] if tokens > 1 else H * D
 
 
 def _positions(positions, freqs, tokens: int, D: int) -> int:
     """rotary_dim, after checks of what the angles are made of."""
     if positions.shape != (tokens,) or not positions.is_contiguous():
         raise ValueError(f"optgqa: positions must be a dense tensor of {tokens} values")
-    if freqs.dim() != 1 or not freqs.is_contiguous() or not 0 < 2 * freqs.shape[0] <= D:
+    shape = freqs.shape
+    if len(shape) != 1 or not freqs.is_contiguous() or not 0 < 2 * shape[0] <= D:
         raise ValueError(f"optgqa: freqs must be a dense tensor of 1 to {D // 2} values")
-    return 2 * freqs.shape[0]
+    return 2 * shape[0]
 
 
 def rotary_embedding(q_out: torch.Tensor, q: torch.Tensor, k_out: Optional[torch.Tensor], k: Optional[torch.Tensor],
@@ -79,44 +112,50 @@ def rotary_embedding(q_out: torch.Tensor, q: torch.Tensor, k_out: Optional[torch
     lib = _pkg.load_library()
     if (k is None) != (k_out is None):
         raise ValueError("optgqa: k and k_out come together")
-    _pkg._typed(q, same=(("q_out", q_out), ("k", k), ("k_out", k_out)), i32=(("positions", positions),), f64=(("freqs", freqs),))
+    code, dtype = _pkg._dtype_code(q), q.dtype
+    tensors = (q, "q", dtype), (q_out, "q_out", dtype), (positions, "positions", torch.int32), (freqs, "freqs", torch.float64)
+    _check_tensors(q.get_device(), tensors if k is None else (*tensors, (k, "k", dtype), (k_out, "k_out", dtype)))
     T, D = q.shape[0], q.shape[-1]
-    Hq, qs = _rows(q, "q", T)
-    if q_out.shape != q.shape or (k is not None and (k_out.shape != k.shape or k.shape[-1] != D)):
-        raise ValueError("optgqa: shape mismatch between q, k and their outputs")
-    qos = _rows(q_out, "q_out", T)[1]
-    Hkv, ks, kos = 0, 0, 0
+    Hq, qs = _rows(q, "q", T, D)
+    Ho, qos = _rows(q_out, "q_out", T, D)
+    Hkv = Hko = ks = kos = 0
     if k is not None:
-        Hkv, ks = _rows(k, "k", T)
-        kos = _rows(k_out, "k_out", T)[1]
+        Hkv, ks = _rows(k, "k", T, D)
+        Hko, kos = _rows(k_out, "k_out", T, D)
+    if Ho != Hq or Hko != Hkv:
+        raise ValueError("optgqa: shape mismatch between q, k and their outputs")
     rot = _positions(positions, freqs, T, D)
     rc = lib.optgqa_rotary_embedding(q_out.data_ptr(), q.data_ptr(), _pkg._ptr(k_out), _pkg._ptr(k), positions.data_ptr(), freqs.data_ptr(),
-                                     T, Hq, Hkv, D, rot, bool(interleaved), magnitude, bool(backward), qos, qs, kos, ks,
-                                     _pkg._dtype_code(q), _pkg._stream(stream))
-    _pkg._check(rc, "optgqa_rotary_embedding")
+                                     T, Hq, Hkv, D, rot, interleaved, magnitude, backward, qos, qs, kos, ks, code, _pkg._stream(stream))
+    if rc:
+        _pkg._check(rc, "optgqa_rotary_embedding")
 
 
 def _append(name, q_out, q, k, v, k_cache, v_cache, slot_mapping, positions, freqs, interleaved, magnitude, stream, kv8, scales) -> None:
     lib = _pkg.load_library()
-    caches = (("k_cache", k_cache), ("v_cache", v_cache))
-    rows = (("q_out", q_out), ("k", k), ("v", v))
-    _pkg._typed(q, same=rows if kv8 else rows + caches, u8=caches if kv8 else (), i32=(("positions", positions),),
-                i64=(("slot_mapping", slot_mapping),), f64=(("freqs", freqs),))
+    code, dtype = _pkg._dtype_code(q), q.dtype
+    cache = torch.uint8 if kv8 else dtype
+    _check_tensors(q.get_device(), ((q, "q", dtype), (q_out, "q_out", dtype), (k, "k", dtype), (v, "v", dtype), (k_cache, "k_cache", cache),
+                                    (v_cache, "v_cache", cache), (positions, "positions", torch.int32),
+                                    (slot_mapping, "slot_mapping", torch.int64), (freqs, "freqs", torch.float64)))
     T, D = q.shape[0], q.shape[-1]
-    NB, Hkv, bs, Dk = k_cache.shape
-    Hq, qs = _rows(q, "q", T)
-    if Dk != D or v_cache.shape != k_cache.shape or q_out.shape != q.shape or k.shape[1:] != (Hkv, D) or v.shape[1:] != (Hkv, D):
+    shape = k_cache.shape
+    NB, Hkv, bs, Dk = shape
+    Hq, qs = _rows(q, "q", T, D)
+    Ho, qos = _rows(q_out, "q_out", T, D)
+    Hk, ks = _rows(k, "k", T, D)
+    Hv, vs = _rows(v, "v", T, D)
+    if Dk != D or v_cache.shape != shape or Ho != Hq or Hk != Hkv or Hv != Hkv:
         raise ValueError("optgqa: shape mismatch between q, q_out, k, v and the caches")
     if slot_mapping.shape != (T,):
         raise ValueError(f"optgqa: slot_mapping must have {T} values")
-    for t, n in ((k_cache, "k_cache"), (v_cache, "v_cache"), (slot_mapping, "slot_mapping")):
-        _pkg._dense(t, n)
-    qos, ks, vs = _rows(q_out, "q_out", T)[1], _rows(k, "k", T)[1], _rows(v, "v", T)[1]
+    _dense((k_cache, "k_cache"), (v_cache, "v_cache"), (slot_mapping, "slot_mapping"))
     rot = _positions(positions, freqs, T, D)
     rc = getattr(lib, name)(q_out.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
-                            slot_mapping.data_ptr(), positions.data_ptr(), freqs.data_ptr(), T, Hq, Hkv, D, rot, bool(interleaved),
-                            magnitude, bs, qos, qs, ks, vs, *scales, _pkg._dtype_code(q), _pkg._stream(stream))
-    _pkg._check(rc, name)
+                            slot_mapping.data_ptr(), positions.data_ptr(), freqs.data_ptr(), T, Hq, Hkv, D, rot, interleaved,
+                            magnitude, bs, qos, qs, ks, vs, *scales, code, _pkg._stream(stream))
+    if rc:
+        _pkg._check(rc, name)
 
 
 def rotary_and_cache(q_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor,
@@ -155,25 +194,34 @@ def common_prefix_workspace_bytes(num_tokens: int, num_seqs: int, num_heads: int
 def _common(name, out, q, k_cache, v_cache, prefix_table, block_tables, context_lens, cu_q_lens, alibi_slopes, scale, max_context_len,
             max_q_len, workspace, stream, kv8, scales) -> None:
     lib = _pkg.load_library()
-    _pkg._attn_typed(q, out, k_cache, v_cache, block_tables, context_lens, alibi_slopes, kv8=kv8, cu_q_lens=cu_q_lens)
-    _pkg._typed(q, i32=(("prefix_table", prefix_table),))
+    code, dtype = _pkg._dtype_code(q), q.dtype
+    cache, i32 = torch.uint8 if kv8 else dtype, torch.int32
+    index = q.get_device()
+    more = () if cu_q_lens is None else ((cu_q_lens, "cu_q_lens", i32),)
+    if alibi_slopes is not None:
+        more += ((alibi_slopes, "alibi_slopes", torch.float32),)
+    _check_tensors(index, ((q, "q", dtype), (out, "out", dtype), (k_cache, "k_cache", cache), (v_cache, "v_cache", cache),
+                           (prefix_table, "prefix_table", i32), (block_tables, "block_tables", i32), (context_lens, "context_lens", i32), *more))
+    shape, tables = k_cache.shape, block_tables.shape
     T, Hq, D = q.shape
-    NB, Hkv, bs, Dk = k_cache.shape
+    NB, Hkv, bs, Dk = shape
     B = context_lens.shape[0]
-    if (Dk != D or out.shape != q.shape or v_cache.shape != k_cache.shape or prefix_table.dim() != 1 or block_tables.dim() != 2
-            or block_tables.shape[0] != B or (T != B if cu_q_lens is None else cu_q_lens.shape != (B + 1,))
-            or (alibi_slopes is not None and alibi_slopes.shape != (Hq,))):
+    if (Dk != D or out.shape != q.shape or v_cache.shape != shape or len(prefix_table.shape) != 1 or len(tables) != 2 or tables[0] != B
+            or (T != B if cu_q_lens is None else cu_q_lens.shape != (B + 1,)) or (alibi_slopes is not None and alibi_slopes.shape != (Hq,))):
         raise ValueError("optgqa: shape mismatch between q, out, the tables, lengths, slopes and the caches")
-    for t, n in ((out, "out"), (q, "q"), (k_cache, "k_cache"), (v_cache, "v_cache"), (prefix_table, "prefix_table"),
-                 (block_tables, "block_tables"), (context_lens, "context_lens"), (cu_q_lens, "cu_q_lens"), (alibi_slopes, "alibi_slopes")):
-        if t is not None:
-            _pkg._dense(t, n)
+    _dense((out, "out"), (q, "q"), (k_cache, "k_cache"), (v_cache, "v_cache"), (prefix_table, "prefix_table"), (block_tables, "block_tables"),
+           (context_lens, "context_lens"))
+    if cu_q_lens is not None:
+        _dense((cu_q_lens, "cu_q_lens"))
+    if alibi_slopes is not None:
+        _dense((alibi_slopes, "alibi_slopes"))
     ws_bytes = _pkg._workspace(workspace, q)
     rc = getattr(lib, name)(out.data_ptr(), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), prefix_table.data_ptr(),
                             block_tables.data_ptr(), context_lens.data_ptr(), _pkg._ptr(cu_q_lens), _pkg._ptr(alibi_slopes), scale, *scales,
-                            T, B, Hq, Hkv, D, bs, prefix_table.shape[0], block_tables.shape[1], max_context_len, max_q_len,
-                            _pkg._ptr(workspace), ws_bytes, _pkg._dtype_code(q), _pkg._stream(stream))
-    _pkg._check(rc, name)
+                            T, B, Hq, Hkv, D, bs, prefix_table.shape[0], tables[1], max_context_len, max_q_len,
+                            _pkg._ptr(workspace), ws_bytes, code, _pkg._stream(stream))
+    if rc:
+        _pkg._check(rc, name)
 
 
 def paged_attention_common(out: torch.Tensor, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, prefix_table: torch.Tensor,
@@ -220,37 +268,33 @@ def verify_drafts(tokens: torch.Tensor, num_accepted: torch.Tensor, target_probs
     """optgqa_verify_drafts: which of the drafts are kept, and each sequence's next token.  tokens [B, max_drafts + 1] int64,
     target_probs [drafts + B, V] and draft_probs [drafts, V] (or None: drafts were certain) float32, float16 or bfloat16."""
     lib = _pkg.load_library()
-    if target_probs.dtype not in _PROBABILITIES:
+    code = _PROBABILITIES.get(target_probs.dtype)
+    if code is None:
         raise TypeError(f"optgqa: probabilities must be float32, float16 or bfloat16, got {target_probs.dtype}")
-    if draft_probs is not None and draft_probs.dtype != target_probs.dtype:
-        raise TypeError(f"optgqa: draft_probs must be {target_probs.dtype}, got {draft_probs.dtype}")
-    index = target_probs.get_device()
-    for t, name, want in ((tokens, "tokens", torch.int64), (num_accepted, "num_accepted", torch.int32), (draft_tokens, "draft_tokens", torch.int64),
-                          (cu_draft_lens, "cu_draft_lens", torch.int32), (accept_uniforms, "accept_uniforms", torch.float32),
-                          (sample_uniforms, "sample_uniforms", torch.float32)):
-        if t.dtype != want:
-            raise TypeError(f"optgqa: {name} must be {want}, got {t.dtype}")
-        if not t.is_cuda or t.get_device() != index or not t.is_contiguous():
-            raise ValueError(f"optgqa: {name} must be a dense tensor on the probabilities' GPU")
-    if draft_probs is not None and draft_probs.get_device() != index:
-        raise ValueError("optgqa: draft_probs must be on the same GPU as target_probs")
-    B, T = num_accepted.shape[0], draft_tokens.shape[0]
-    if target_probs.dim() != 2 or tokens.dim() != 2:
+    index, i64, i32, f32 = target_probs.get_device(), torch.int64, torch.int32, torch.float32
+    draft = () if draft_probs is None else ((draft_probs, "draft_probs", target_probs.dtype),)
+    _check_tensors(index, (*draft, (tokens, "tokens", i64), (num_accepted, "num_accepted", i32), (draft_tokens, "draft_tokens", i64),
+                           (cu_draft_lens, "cu_draft_lens", i32), (accept_uniforms, "accept_uniforms", f32), (sample_uniforms, "sample_uniforms", f32)))
+    _dense((tokens, "tokens"), (num_accepted, "num_accepted"), (draft_tokens, "draft_tokens"), (cu_draft_lens, "cu_draft_lens"),
+           (accept_uniforms, "accept_uniforms"), (sample_uniforms, "sample_uniforms"))
+    B, T, wide, rows = num_accepted.shape[0], draft_tokens.shape[0], tokens.shape, target_probs.shape
+    if len(rows) != 2 or len(wide) != 2:
         raise ValueError("optgqa: tokens and target_probs must have two dimensions")
-    V = target_probs.shape[1]
-    if (tokens.shape[0] != B or tokens.shape[1] < 1 or target_probs.shape[0] != T + B or cu_draft_lens.shape != (B + 1,)
-            or accept_uniforms.shape != (T,) or sample_uniforms.shape != (B,) or (draft_probs is not None and draft_probs.shape != (T, V))):
+    V = rows[1]
+    if (wide[0] != B or wide[1] < 1 or rows[0] != T + B or cu_draft_lens.shape != (B + 1,) or accept_uniforms.shape != (T,)
+            or sample_uniforms.shape != (B,) or (draft_probs is not None and draft_probs.shape != (T, V))):
         raise ValueError("optgqa: shape mismatch between the tokens, probabilities, drafts and random numbers")
-    for t, name in ((target_probs, "target_probs"), (draft_probs, "draft_probs")):
-        if t is not None and t.shape[0] and t.stride(1) != 1 and V > 1:
-            raise ValueError(f"optgqa: {name} must have dense rows")
+    target_stride, draft_stride = _row_stride(target_probs, "target_probs"), 0 if draft_probs is None else _row_stride(draft_probs, "draft_probs")
     ws_bytes = _pkg._workspace(workspace, target_probs)
     rc = lib.optgqa_verify_drafts(tokens.data_ptr(), num_accepted.data_ptr(), target_probs.data_ptr(), _pkg._ptr(draft_probs),
                                   draft_tokens.data_ptr(), cu_draft_lens.data_ptr(), accept_uniforms.data_ptr(), sample_uniforms.data_ptr(),
-                                  B, V, tokens.shape[1] - 1, _row_stride(target_probs), 0 if draft_probs is None else _row_stride(draft_probs),
-                                  _pkg._ptr(workspace), ws_bytes, _PROBABILITIES[target_probs.dtype], _pkg._stream(stream))
-    _pkg._check(rc, "optgqa_verify_drafts")
+                                  B, V, wide[1] - 1, target_stride, draft_stride, _pkg._ptr(workspace), ws_bytes, code, _pkg._stream(stream))
+    if rc:
+        _pkg._check(rc, "optgqa_verify_drafts")
 
 
-def _row_stride(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+def _row_stride(t: torch.Tensor, name: str) -> int:
+    stride, shape = t.stride(), t.shape
+    if shape[0] and shape[1] > 1 and stride[1] != 1:
+        raise ValueError(f"optgqa: {name} must have dense rows")
+    return stride[0] if shape[0] > 1 else shape[1]

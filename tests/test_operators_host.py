@@ -167,3 +167,27 @@ def test_common_prefix_workspace_covers_every_smaller_call(G):
     for T, B, Hq, Hkv, D, NP, Lmax, n in ((9, 9, 32, 8, 128, 100, 5000, 9), (64, 64, 32, 4, 128, 0, 4000, 5), (600, 64, 8, 8, 64, 1000, 20000, 100)):
         big = G.common_prefix_workspace_bytes(T, B, Hq, Hkv, D, 16, NP, Lmax, n)
         assert big >= G.common_prefix_workspace_bytes(T, B, Hq, Hkv, D, 16, NP, Lmax, 1)
+
+
+def test_types_are_refused_before_places(G):
+    """CPU tensors throughout: a wrong type is a TypeError, right types a ValueError."""
+    import torch
+    i32, i64 = torch.zeros(3, dtype=torch.int32), torch.zeros(3, dtype=torch.int64)
+    h, c = torch.zeros(3, 4, 64, dtype=torch.float16), torch.zeros(2, 2, 16, 64, dtype=torch.float16)
+    kv, f = torch.zeros(3, 2, 64, dtype=torch.float16), torch.zeros(32, dtype=torch.float64)
+    bt, ws = torch.zeros(3, 4, dtype=torch.int32), torch.zeros(64, dtype=torch.uint8)
+    good = {G.rotary_and_cache: [h, h, kv, kv, c, c, i64, i32, f], G.paged_attention_common: [h, h, c, c, i32, bt, i32, None, None, 0.1, 100, 1, ws],
+            G.rotary_and_cache_fp8: [h, h, kv, kv, c.byte(), c.byte(), i64, i32, f, 1.0, 1.0],
+            G.paged_attention_common_fp8: [h, h, c.byte(), c.byte(), i32, bt, i32, None, torch.zeros(4), 0.1, 1.0, 1.0, 100, 1, ws],
+            G.verify_drafts: [torch.zeros(3, 3, dtype=torch.int64), i32, torch.zeros(6, 50), torch.zeros(3, 50), i64, torch.zeros(4, dtype=torch.int32),
+                              torch.zeros(3), torch.zeros(3), ws]}
+    for call, args in good.items():
+        with pytest.raises(ValueError):
+            call(*args)
+        for i, x in enumerate(args):
+            if not isinstance(x, torch.Tensor) or x is ws:
+                continue
+            with pytest.raises(TypeError):
+                call(*args[:i], x.to(torch.complex64), *args[i + 1:])
+            with pytest.raises((TypeError, AttributeError)):
+                call(*args[:i], np.zeros(3), *args[i + 1:])
