@@ -145,11 +145,12 @@ int rotary_and_cache_impl(void* q_out, const void* q, const void* k, const void*
     return rotary_impl(c, scales ? RotaryTo::kCacheE4M3 : RotaryTo::kCache, static_cast<hipStream_t>(stream));
 }
 
-template <int DT, int VEC>
+template <int DT>
 int launch_verify(const VerifyParams& a, int num_seqs, hipStream_t st)
 {
-    const int rc = launch(verify_sums_kernel<DT, VEC>, dim3(num_seqs, a.chunks), dim3(kVerifyThreads), 0, st, a);
-    return rc != OPTGQA_OK ? rc : launch(verify_select_kernel<DT, VEC>, dim3(num_seqs), dim3(kVerifyThreads), 0, st, a);
+    constexpr int kWaves = kVerifyThreads / 64;
+    const int rc = launch(verify_sums_kernel<DT>, dim3(num_seqs, (a.chunks + kWaves - 1) / kWaves), dim3(kVerifyThreads), 0, st, a);
+    return rc != OPTGQA_OK ? rc : launch(verify_select_kernel<DT>, dim3(num_seqs), dim3(64), 0, st, a);
 }
 
 // How a common-prefix call is cut into pieces; the same for its workspace and its launch.
@@ -393,7 +394,7 @@ int optgqa_rotary_and_cache_fp8_heads(void* q_out, const void* q, const void* k,
 size_t optgqa_verify_drafts_workspace_bytes(int num_seqs, int vocab_size)
 {
     if (num_seqs <= 0 || vocab_size <= 0) return 0;
-    return (size_t)num_seqs * 2 * (((size_t)vocab_size + kVerifyChunk - 1) / kVerifyChunk) * sizeof(double);
+    return (size_t)num_seqs * (((size_t)vocab_size + kVerifyChunk - 1) / kVerifyChunk * sizeof(double2) + sizeof(Verdict));
 }
 
 int optgqa_verify_drafts(int64_t* tokens, int32_t* num_accepted, const void* target_probs, const void* draft_probs,
@@ -405,7 +406,7 @@ int optgqa_verify_drafts(int64_t* tokens, int32_t* num_accepted, const void* tar
         return OPTGQA_ERR_SHAPE;
     if (!dtype_ok(dtype) && dtype != OPTGQA_F32) return OPTGQA_ERR_UNSUPPORTED;
     const int chunks = (int)(((int64_t)vocab_size + kVerifyChunk - 1) / kVerifyChunk);
-    if (chunks > 65535) return OPTGQA_ERR_SHAPE;                 // (2^28 entries)
+    if (chunks > 4 * 65535) return OPTGQA_ERR_SHAPE;             // (2^28 entries)
     if (num_seqs == 0) return OPTGQA_OK;
     if (!tokens || !num_accepted || !target_probs || !cu_draft_lens || !sample_uniforms)
         return OPTGQA_ERR_NULL;
@@ -424,7 +425,8 @@ int optgqa_verify_drafts(int64_t* tokens, int32_t* num_accepted, const void* tar
     a.cu = cu_draft_lens;
     a.accept_u = accept_uniforms;
     a.sample_u = sample_uniforms;
-    a.sums = static_cast<double*>(workspace);
+    a.sums = static_cast<double2*>(workspace);
+    a.verdicts = reinterpret_cast<Verdict*>(a.sums + (size_t)num_seqs * chunks);
     a.target_stride = target_stride;
     a.draft_stride = draft_stride;
     a.vocab = vocab_size;
@@ -432,11 +434,8 @@ int optgqa_verify_drafts(int64_t* tokens, int32_t* num_accepted, const void* tar
     a.looked_at = draft_tokens && accept_uniforms ? max_drafts : 0;
     a.chunks = chunks;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    // 16-byte loads where every row lies on 16 bytes
-    const bool wide = !(rows & 15u) && (target_stride | (draft_probs ? draft_stride : 0)) % (int64_t)(16 / size) == 0;
-    if (dtype == OPTGQA_F32) return wide ? launch_verify<kF32, 4>(a, num_seqs, st) : launch_verify<kF32, 1>(a, num_seqs, st);
-    if (dtype == OPTGQA_F16) return wide ? launch_verify<kF16, 8>(a, num_seqs, st) : launch_verify<kF16, 1>(a, num_seqs, st);
-    return wide ? launch_verify<kBF16, 8>(a, num_seqs, st) : launch_verify<kBF16, 1>(a, num_seqs, st);
+    if (dtype == OPTGQA_F32) return launch_verify<kF32>(a, num_seqs, st);
+    return dtype == OPTGQA_F16 ? launch_verify<kF16>(a, num_seqs, st) : launch_verify<kBF16>(a, num_seqs, st);
 }
 
 size_t optgqa_common_prefix_workspace_bytes(int num_tokens, int num_seqs, int num_heads, int num_kv_heads, int head_dim,
