@@ -117,10 +117,11 @@ int rotary_impl(const RotaryCall& c, RotaryTo to, hipStream_t st)
     p.pieces_shift = __builtin_ctz(c.head_dim / (wide ? 16 : 2));
     p.block_shift = store ? __builtin_ctz(c.block_size) : 0;
 
-    // Many tokens: whole tokens, up to 8, some 1 500 items for a workgroup's 256 threads, so that a token's angles are worked
-    // out once.  Fewer than that makes four workgroups to a CU: one token each, its heads dealt to workgroups of one item a thread.
+    // Many tokens: whole tokens, up to 8, as many as make 512 items for a workgroup's 256 threads, so that a token's angles are
+    // worked out once (512: 20 480 tokens of 40 heads of 128 76 us; 1 536: 81, 3 000: 86).  Fewer than four such workgroups to
+    // a CU: one token each, its heads dealt to workgroups of one item a thread.
     const int64_t per_token = (int64_t)p.heads << p.pieces_shift;
-    p.tokens_per_wg = (int)std::min<int64_t>(std::max<int64_t>(1536 / per_token, 1), kRotaryMaxTokens);
+    p.tokens_per_wg = (int)std::min<int64_t>(std::max<int64_t>(512 / per_token, 1), kRotaryMaxTokens);
     p.heads_per_wg = p.heads;
     if (c.num_tokens < (int64_t)4 * num_cus() * p.tokens_per_wg) {
         p.tokens_per_wg = 1;
