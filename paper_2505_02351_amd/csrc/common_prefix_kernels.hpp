@@ -25,7 +25,26 @@
 namespace optgqa {
 
 constexpr int kCommonThreads = 256, kCommonWaves = 4;
-constexpr int kCommonBuffers = 4;               // tile buffers (a K and a V tile) of a workgroup, over its key groups
+
+// A tile of 32 keys in LDS, as the memory system writes it (see PfDirect): 2-byte rows, or 8-bit codes as they are.  Rows of as many
+// bytes lie alike; the 64 bytes of a row of 64 codes, 16 rows to a group, with their columns of 16 bytes exchanged by
+// row, so that a column of 16 rows again lies in 16 different sixteenths of the banks.
+template <int D, bool KV8> struct CommonTile {
+    static constexpr bool kShort = KV8 && D == 64;
+    static constexpr int kRowBytes = KV8 ? D : 2 * D;
+    typedef PfDirect<kShort ? 64 : kRowBytes / 2> Like;
+    static constexpr int kRows = 1024 / kRowBytes, kGroups = kPfKeys / kRows;
+    static constexpr int kGroup = kShort ? 1024 + 64 : Like::kGroup, kTile = kGroups * kGroup;
+    static constexpr int kBuffers = KV8 ? 8 : 4;                 // of a K and a V tile, of a workgroup, over its key groups
+    static __device__ __forceinline__ int load_row(int l) { return kShort ? l >> 2 : Like::load_row(l); }
+    static __device__ __forceinline__ int load_col(int l) { return kShort ? (l & 3) ^ ((l >> 4) & 3) : Like::load_col(l); }
+    // byte offset of a row's 16-byte column 0 or 1, and of the one 2m further on
+    static __device__ __forceinline__ int at(int row, int col)
+    {
+        return kShort ? (row >> 4) * kGroup + (row & 15) * 64 + ((col ^ ((row >> 2) & 3)) << 4) : Like::row_at(row, col);
+    }
+    static __device__ __forceinline__ int further(int at, int m) { return kShort ? at ^ (32 * m) : at + Like::dims_at(m); }
+};
 
 struct CommonParams {
     void* out;                  // [T][Hq][D]
@@ -52,8 +71,8 @@ struct CommonParams {
     FastDiv by_group, by_p_tiles, by_kv_heads, by_s_shares;
 };
 
-template <int D> constexpr int kCommonLds = [] {
-    const int tiles = kCommonBuffers * 2 * PfDirect<D>::kTile, join = kCommonWaves * 64 * (D / 8 * 16 + 8);
+template <int D, bool KV8> constexpr int kCommonLds = [] {
+    const int tiles = CommonTile<D, KV8>::kBuffers * 2 * CommonTile<D, KV8>::kTile, join = kCommonWaves * 64 * (D / 8 * 16 + 8);
     return tiles > join ? tiles : join;
 }();
 
@@ -161,14 +180,16 @@ struct CommonJob {
     int held_first, held;       // the lane's entry of `table`: held_first + lane
 };
 
-template <int DT> __device__ __forceinline__ bool any_not_finite(uint4 x)
+// of 16 bytes of values, or of codes (whose only such value is NaN)
+template <int DT, bool KV8> __device__ __forceinline__ bool any_not_finite(uint4 x)
 {
     constexpr uint32_t kExp = DT == kF16 ? 0x7c00u : 0x7f80u;
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t w = i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w;
-        odd = odd || (w & kExp) == kExp || ((w >> 16) & kExp) == kExp;
+        if (KV8) odd = odd || (w & 0x7fu) == 0x7fu || (w & 0x7f00u) == 0x7f00u || (w & 0x7f0000u) == 0x7f0000u || (w & 0x7f000000u) == 0x7f000000u;
+        else odd = odd || (w & kExp) == kExp || ((w >> 16) & kExp) == kExp;
     }
     return odd;
 }
@@ -185,14 +206,16 @@ template <int DT> __device__ __forceinline__ uint32_t finite_pair(uint32_t w)
 template <int DT, bool KV8, int D, int RW>
 __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJob& job)
 {
-    constexpr int KS = kCommonWaves / RW, NBUF = kCommonBuffers / KS;
+    constexpr int KS = kCommonWaves / RW;
     constexpr int kQ = D / 16, kDB = D / 32, kPieces = D / 8;
     constexpr int ES = KV8 ? 1 : 2;
-    typedef PfDirect<D> Tile;
-    constexpr int kWaveGroups = Tile::kGroups / RW;              // 1 KiB groups of a K (or V) tile that a wave brings
-    constexpr int kHalves = RW == 1 ? 2 : 1;                     // runs of up to 16 keys, each in one block, they lie in
+    typedef CommonTile<D, KV8> Tile;
+    constexpr int NBUF = Tile::kBuffers / KS > 4 ? 4 : Tile::kBuffers / KS;
+    constexpr bool kHalfLoad = Tile::kGroups < RW;               // fewer 1 KiB groups than waves: half of them bring K, half V
+    constexpr int kWaveGroups = kHalfLoad ? 1 : Tile::kGroups / RW;              // groups of a K (or V) tile that a wave brings
+    constexpr int kWaveKeys = kWaveGroups * Tile::kRows;
+    constexpr int kHalves = kWaveKeys > 16 ? 2 : 1;              // runs of up to 16 keys, each in one block, they lie in
     constexpr int kRunGroups = kWaveGroups / kHalves;
-    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
     extern __shared__ __attribute__((aligned(16))) unsigned char common_lds[];
     unsigned char* const lds = common_lds;
     const int lane = threadIdx.x & 63, n32 = lane & 31, h2 = lane >> 5;
@@ -206,9 +229,10 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
     const int t = job.tok0 + ti;
     uint4 qb[kQ];
     {
-        const unsigned char* const qp = static_cast<const unsigned char*>(p.q) + ((int64_t)t * p.num_heads + head) * (D * 2) + 16 * h2;
+        // (the lane's dims of score MFMA m: 16m + 8 h2 .. + 7; of codes, 16 of which are one read: 32 (m / 2) + 16 h2 + 8 (m % 2) ..)
+        const unsigned char* const qp = static_cast<const unsigned char*>(p.q) + ((int64_t)t * p.num_heads + head) * (D * 2) + (KV8 ? 32 : 16) * h2;
 #pragma unroll
-        for (int m = 0; m < kQ; ++m) qb[m] = *reinterpret_cast<const uint4*>(qp + 32 * m);
+        for (int m = 0; m < kQ; ++m) qb[m] = *reinterpret_cast<const uint4*>(qp + (KV8 ? 64 * (m >> 1) + 16 * (m & 1) : 32 * m));
     }
     float slope = p.slopes ? p.slopes[head] : 0.f;
     int pos = job.pos0 + ti;
@@ -224,7 +248,7 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
     const int last_block = (kend - 1) >> bshift;
     int held_first = job.held_first, held = job.held;
     const int load_row = Tile::load_row(lane), load_col = Tile::load_col(lane);
-    const uint32_t lane_off = (uint32_t)(load_row * D * ES + 8 * load_col * ES);
+    const uint32_t lane_off = (uint32_t)(load_row * Tile::kRowBytes + 16 * load_col);
     // byte offset, in either cache from its KV head's first block on, of key `key` (wave-uniform)
     auto key_at = [&](int key) __attribute__((always_inline)) -> uint64_t {
         const int block = key >> bshift;
@@ -233,74 +257,63 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
             held = job.table[min(held_first + lane, last_block)];
             asm volatile("" : "+v"(held));                       // (waited for here, not on the way that reads no table)
         }
-        return (uint64_t)(uint32_t)__builtin_amdgcn_readlane(held, block - held_first) * blk_bytes + (uint32_t)((key & bmask) * (D * ES));
+        return (uint64_t)(uint32_t)__builtin_amdgcn_readlane(held, block - held_first) * blk_bytes + (uint32_t)((key & bmask) * Tile::kRowBytes);
     };
-    // offsets, and this lane's, of the wave's runs of the group's tile j
+    // offsets, and this lane's, of the wave's runs of the group's tile j; `first`: its first 1 KiB group of the tile
+    const int first_k = kHalfLoad ? rw : rw * kWaveGroups, first_v = kHalfLoad ? rw - (RW - Tile::kGroups) : first_k;
     struct Runs { uint64_t at[kHalves]; uint32_t lane_at[kWaveGroups]; };
-    auto runs_of = [&](int j) __attribute__((always_inline)) {
+    auto runs_of = [&](int j, int first_group) __attribute__((always_inline)) {
         Runs r;
-        const int key0 = kbeg + kPfKeys * (j * KS + kw) + rw * (kPfKeys / RW);
-        const bool tail = key0 + kPfKeys / RW > kend;            // keys from kend on: kend - 1 again
+        const int key0 = kbeg + kPfKeys * (j * KS + kw) + first_group * Tile::kRows;
+        const bool tail = key0 + kWaveKeys > kend;               // keys from kend on: kend - 1 again
 #pragma unroll
         for (int h = 0; h < kHalves; ++h) r.at[h] = key_at(min(key0 + 16 * h, kend - 1));
 #pragma unroll
         for (int n = 0; n < kWaveGroups; ++n) {
-            r.lane_at[n] = (uint32_t)((n % kRunGroups) * Tile::kRows * D * ES) + lane_off;
+            r.lane_at[n] = (uint32_t)((n % kRunGroups) * 1024) + lane_off;
             if (tail) {
                 const int first = min(key0 + 16 * (n / kRunGroups), kend - 1);
                 const int key = min(key0 + n * Tile::kRows + load_row, kend - 1);
-                r.lane_at[n] = (uint32_t)((key - first) * (D * ES) + 8 * load_col * ES);
+                r.lane_at[n] = (uint32_t)((key - first) * Tile::kRowBytes + 16 * load_col);
             }
         }
         return r;
     };
     auto buffer = [&](int j) __attribute__((always_inline)) { return (kw * NBUF + (j & (NBUF - 1))) * 2 * Tile::kTile; };     // K tile, then V tile
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
-    // 2-byte caches: straight to LDS
-    auto ask = [&](const Runs& r, const unsigned char* cache, int at) __attribute__((always_inline)) {
+    // (of the wave's groups; nothing for a wave that does not bring this tensor)
+    auto ask = [&](const Runs& r, const unsigned char* cache, int at, int first_group) __attribute__((always_inline)) {
 #pragma unroll
         for (int n = 0; n < kWaveGroups; ++n) {
-            const uint32_t to = lds0 + at + (rw * kWaveGroups + n) * Tile::kGroup;
+            const uint32_t to = lds0 + at + (first_group + n) * Tile::kGroup;
             if (RW == 1) stream_direct(to, cache + r.at[n / kRunGroups], r.lane_at[n]);      // (no other row tile reads them)
             else load_direct(to, cache + r.at[n / kRunGroups], r.lane_at[n]);
         }
-    };
-    // 8-bit caches: codes to registers, widened on the way into LDS
-    u32x2 stage_k[KV8 ? kWaveGroups : 1], stage_v[KV8 ? kWaveGroups : 1];
-    auto fetch = [&](const Runs& r, const unsigned char* cache, u32x2* stage) __attribute__((always_inline)) {
-#pragma unroll
-        for (int n = 0; n < kWaveGroups; ++n)
-            stage[n] = *reinterpret_cast<const u32x2*>(cache + r.at[n / kRunGroups] + r.lane_at[n]);
-    };
-    auto put = [&](const u32x2* stage, int at) __attribute__((always_inline)) {
-#pragma unroll
-        for (int n = 0; n < kWaveGroups; ++n)
-            *reinterpret_cast<uint4*>(lds + at + (rw * kWaveGroups + n) * Tile::kGroup + 16 * lane) = widen8_e4m3<DT>(stage[n][0], stage[n][1]);
     };
 
     // ---- the first tiles -------------------------------------------------------------------------------------
     // RW > 1: a key group's K and V tiles in rings of NBUF buffers.  The scores of a step's tile are made a step ahead, under the
     // softmax of the tile before, so K tiles run one ahead of V tiles: step j asks for K tile j + 1 + kLead and V tile j + kLead.
-    // RW == 1: a wave's own tiles, one buffer: the next K tile is asked for when this one's scores are there, the next V
-    // tile when this one's output is.
+    // RW == 1: a wave's own tiles, NBUF buffers: K tile j + NBUF is asked for when the scores of tile j are there, its V
+    // tile when the output of tile j is.
     constexpr int kLead = NBUF / 2;
-    constexpr int kLoads = 2 * kWaveGroups;                      // of a wave, per K and V tile
+    constexpr int kLoads = kHalfLoad ? 1 : 2 * kWaveGroups;      // of a wave, per K and V tile
     auto buffer_v = [&](int j) __attribute__((always_inline)) { return buffer(j) + Tile::kTile; };
-    const int at_k = buffer(0), at_v = at_k + Tile::kTile;       // (RW == 1)
-    auto ask_k = [&](int j) __attribute__((always_inline)) { if (has(j)) ask(runs_of(j), kc, buffer(j)); };
-    auto ask_v = [&](int j) __attribute__((always_inline)) { if (has(j)) ask(runs_of(j), vc, buffer_v(j)); };
+    auto ask_k = [&](int j) __attribute__((always_inline)) {
+        if (has(j) && (!kHalfLoad || first_k < Tile::kGroups)) ask(runs_of(j, first_k), kc, buffer(j), first_k);
+    };
+    auto ask_v = [&](int j) __attribute__((always_inline)) {
+        if (has(j) && first_v >= 0) ask(runs_of(j, first_v), vc, buffer_v(j), first_v);
+    };
     asm volatile("" : "+v"(held) :: "memory");
-    if constexpr (KV8) {
-        if (has(0)) {
-            const Runs first = runs_of(0);
-            fetch(first, kc, stage_k);
-            fetch(first, vc, stage_v);
-        }
-    } else {
+    if constexpr (RW > 1) {
         ask_k(0);
-        if constexpr (RW > 1) ask_k(1);
+        ask_k(1);
         ask_v(0);
-        if constexpr (RW > 1 && kLead == 2) ask_k(2), ask_v(1);
+        if constexpr (kLead == 2) ask_k(2), ask_v(1);
+    } else {
+#pragma unroll
+        for (int j = 0; j < NBUF; ++j) ask_k(j), ask_v(j);
     }
     const int lim = row_ok ? min(pos + 1, kend) : kend;          // keys below it are visible
     const int least = -wave_max(-lim);                           // tiles that end at or below it need no mask
@@ -324,17 +337,26 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
     float m_ref = 0.f, lsum = 0.f;
     bool started = !row_ok;
 
-    const int k_at = Tile::row_at(n32, h2);
-    // `between`: what is issued behind the reads of the first four operands (a step's loads to LDS)
+    const int k_at = Tile::at(n32, h2);
+    // `between`: what is issued behind the reads of the first operands (a step's loads to LDS)
     auto scores = [&](int at, auto between) __attribute__((always_inline)) {
+        constexpr int kReads = KV8 ? kQ / 2 : kQ, kEarly = kReads < 4 ? kReads : 4;
         f32x16 st = key_bias;
-        auto read = [&](int m) __attribute__((always_inline)) { return *reinterpret_cast<const uint4*>(lds + at + k_at + Tile::dims_at(m)); };
-        uint4 ka[4];
+        auto read = [&](int m) __attribute__((always_inline)) { return *reinterpret_cast<const uint4*>(lds + at + Tile::further(k_at, m)); };
+        uint4 ka[kEarly];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) ka[m] = read(m);
+        for (int m = 0; m < kEarly; ++m) ka[m] = read(m);
         between();
 #pragma unroll
-        for (int m = 0; m < kQ; ++m) st = mfma32<DT>(m < 4 ? ka[m & 3] : read(m), qb[m], st);
+        for (int m = 0; m < kReads; ++m) {
+            const uint4 x = m < kEarly ? ka[m < kEarly ? m : 0] : read(m);
+            if constexpr (KV8) {
+                st = mfma32<DT>(widen8_e4m3<DT>(x.x, x.y), qb[2 * m], st);
+                st = mfma32<DT>(widen8_e4m3<DT>(x.z, x.w), qb[2 * m + 1], st);
+            } else {
+                st = mfma32<DT>(x, qb[m], st);
+            }
+        }
         return st;
     };
     uint32_t pk[2][4], pk_lo[2][4];                              // weights as pairs of 2-byte values (and what is left of them)
@@ -377,19 +399,31 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
                 // one rounding: the sum is that of the weights as rounded, the output an exact convex combination
                 const uint32_t two = narrow2<DT>(w0, w1);
                 pk[e >> 2][e & 3] = two;
-                lsum += widen_lo<DT>(two) + widen_hi<DT>(two);
+                lsum = dot2<DT>(two, 0x3c003c00u, lsum);         // (times 1, 1: one instruction for a pair)
             }
         }
     };
-    typedef short i16x4 __attribute__((ext_vector_type(4)));
-    typedef __attribute__((address_space(3))) i16x4* lds_i16x4_ptr;
-    const int v_at = Tile::keys_at(lane & 15, (lane >> 4) & 1, h2);
-    // keys 16m + 4 h2 .. + 3 and 16m + 8 + 4 h2 .. + 3 of dim 32 db + n32
+    // V^T: keys 16m + 4 h2 .. + 3 and 16m + 8 + 4 h2 .. + 3 of dim 32 db + n32, by transposing loads, in which lane s of 16 addresses
+    //   2-byte  key s / 4 of four, dims 4 (s % 4) .. + 3, and gets its dim's four keys (two loads);
+    //   codes   key s / 2 of eight (as they lie: four, four behind the next), dims 8 (s % 2) .. + 7, and gets its dim's eight keys.
+    const int s16 = lane & 15, dhalf = (lane >> 4) & 1;
+    int v_at;
+    if constexpr (KV8) v_at = Tile::at(4 * h2 + ((s16 >> 1) & 3) + 8 * (s16 >> 3), dhalf) + 8 * (s16 & 1);
+    else v_at = Tile::Like::keys_at(s16, dhalf, h2);
     auto v_operand = [&](int at, int m, int db) __attribute__((always_inline)) {
-        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_ptr)(lds + at + v_at + Tile::further(2 * m, db)));
-        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_ptr)(lds + at + v_at + Tile::further(2 * m + 1, db)));
-        const uint2 lo2 = __builtin_bit_cast(uint2, lo), hi2 = __builtin_bit_cast(uint2, hi);
-        return make_uint4(lo2.x, lo2.y, hi2.x, hi2.y);
+        if constexpr (KV8) {
+            typedef int i32x2 __attribute__((ext_vector_type(2)));
+            typedef __attribute__((address_space(3))) i32x2* lds_i32x2_ptr;
+            const i32x2 x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2_ptr)(lds + at + Tile::further(v_at + m * (16 / Tile::kRows) * Tile::kGroup, db)));
+            return widen8_e4m3<DT>((uint32_t)x[0], (uint32_t)x[1]);
+        } else {
+            typedef short i16x4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) i16x4* lds_i16x4_ptr;
+            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_ptr)(lds + at + v_at + Tile::Like::further(2 * m, db)));
+            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_ptr)(lds + at + v_at + Tile::Like::further(2 * m + 1, db)));
+            const uint2 lo2 = __builtin_bit_cast(uint2, lo), hi2 = __builtin_bit_cast(uint2, hi);
+            return make_uint4(lo2.x, lo2.y, hi2.x, hi2.y);
+        }
     };
     auto weighted = [&](uint4 va, int m, f32x16 c) __attribute__((always_inline)) {
         c = mfma32<DT>(va, make_uint4(pk[m][0], pk[m][1], pk[m][2], pk[m][3]), c);
@@ -409,7 +443,7 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
         bool odd = false;
 #pragma unroll
         for (int n = 0; n < Tile::kGroups; ++n)
-            odd = odd || (key0 + n * Tile::kRows + load_row >= least && any_not_finite<DT>(*reinterpret_cast<const uint4*>(lds + at + n * Tile::kGroup + 16 * lane)));
+            odd = odd || (key0 + n * Tile::kRows + load_row >= least && any_not_finite<DT, KV8>(*reinterpret_cast<const uint4*>(lds + at + n * Tile::kGroup + 16 * lane)));
         if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) == 0, 1)) {
             output(at);
             return;
@@ -426,7 +460,13 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
             const bool sees = key0 + k < lim;
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {                  // dims 8i + 4 h2 .. + 3
-                const uint2 v = *reinterpret_cast<const uint2*>(lds + at + Tile::row_at(k, i & 1) + Tile::dims_at(i >> 1) + 8 * h2);
+                uint2 v;
+                if constexpr (KV8) {
+                    const uint32_t c = *reinterpret_cast<const uint32_t*>(lds + at + Tile::further(Tile::at(k, (i >> 1) & 1), i >> 2) + 8 * (i & 1) + 4 * h2);
+                    v = make_uint2(widen2_e4m3<DT>(c, false), widen2_e4m3<DT>(c, true));
+                } else {
+                    v = *reinterpret_cast<const uint2*>(lds + at + Tile::further(Tile::at(k, i & 1), i >> 1) + 8 * h2);
+                }
                 const uint32_t bad[2] = {v.x ^ finite_pair<DT>(v.x), v.y ^ finite_pair<DT>(v.y)};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -449,7 +489,7 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
     // different loops: both have the same barriers.)
     const int mine = (ntiles - kw + KS - 1) / KS;                // tiles of this wave's key group
     const int whole = min(mine, max(0, (least - kbeg) / kPfKeys - kw + KS - 1) / KS);
-    if constexpr (RW > 1 && !KV8) {
+    if constexpr (RW > 1) {
         auto step = [&](int j, const f32x16& st_cur, f32x16& st_ahead, auto masked) __attribute__((always_inline)) {
             // K tile j + 1 and V tile j are there; newer: step j - 1's, where it asked for all of its own
             if (kLead > 1 && j + kLead < mine) wait_direct<(kLead - 1) * kLoads>();
@@ -482,60 +522,29 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
             step(j, st, st_other, std::true_type{});
             st = st_other;
         }
-    } else if constexpr (RW > 1) {
-        // 8-bit caches: codes wait in registers while the tile before is worked on
-        auto land = [&](int j) __attribute__((always_inline)) {
-            put(stage_k, buffer(j));
-            put(stage_v, buffer_v(j));
-        };
-        auto bring = [&](int j) __attribute__((always_inline)) {
-            const Runs runs = runs_of(j);
-            fetch(runs, kc, stage_k);
-            fetch(runs, vc, stage_v);
-        };
-        if (has(0)) land(0);
-        if (has(1)) bring(1);
-        auto step = [&](int j, auto masked) __attribute__((always_inline)) {
-            __syncthreads();                                     // tile j is there for all, the buffers of tile j - 1 free
-            if (has(j + 1)) land(j + 1);
-            if (has(j + 2)) bring(j + 2);
-            if (!decltype(masked)::value || j < mine) finish(j, scores(buffer(j), [] {}), buffer_v(j), masked);
-        };
-        int j = 0;
-        for (; j < whole; ++j) step(j, std::false_type{});
-        for (; j < steps; ++j) step(j, std::true_type{});
     } else {
         auto step = [&](int j, auto masked) __attribute__((always_inline)) {
-            const bool more = j + 1 < mine;
-            if constexpr (KV8) {
-                put(stage_k, at_k);
-                put(stage_v, at_v);
-                if (more) {
-                    const Runs runs = runs_of(j + 1);
-                    fetch(runs, kc, stage_k);
-                    fetch(runs, vc, stage_v);
-                }
-                wave_lds_fence();
-                finish(j, scores(at_k, [] {}), at_v, masked);
-                wave_lds_fence();
-            } else {
-                wait_direct<kWaveGroups>();                      // (V tile j is newer)
-                const f32x16 st = scores(at_k, [] {});
-                reads_done();
-                Runs runs;
-                if (more) {
-                    runs = runs_of(j + 1);
-                    ask(runs, kc, at_k);
-                }
-                softmax(first_key(j), st, masked);
-                if (more) wait_direct<kWaveGroups>();
-                else wait_direct();
-                if (decltype(masked)::value) output_cut(first_key(j), at_v);
-                else output(at_v);
-                reads_done();
-                if (more) ask(runs, vc, at_v);
+            // K tile j is there; newer: its V tile and what was asked for since
+            if (NBUF > 1 && j + NBUF - 1 < mine) wait_direct<(2 * NBUF - 1) * kWaveGroups>();
+            else wait_direct<kWaveGroups>();
+            const f32x16 st = scores(buffer(j), [] {});
+            reads_done();
+            const bool more = j + NBUF < mine;
+            Runs runs;
+            if (more) {
+                runs = runs_of(j + NBUF, 0);
+                ask(runs, kc, buffer(j), 0);
             }
+            softmax(first_key(j), st, masked);
+            if (more) wait_direct<(2 * NBUF - 1) * kWaveGroups>();
+            else if (NBUF > 1 && j + 1 < mine) wait_direct<2 * kWaveGroups>();
+            else wait_direct();
+            if (decltype(masked)::value) output_cut(first_key(j), buffer_v(j));
+            else output(buffer_v(j));
+            reads_done();
+            if (more) ask(runs, vc, buffer_v(j), 0);
         };
+        static_assert(NBUF <= 2, "what is newer than a V tile");
         int j = 0;
         for (; j < whole; ++j) step(j, std::false_type{});
         for (; j < mine; ++j) step(j, std::true_type{});
@@ -648,41 +657,43 @@ __global__ __launch_bounds__(kCommonThreads, 2) void common_prefix_kernel(const 
     else common_body<DT, KV8, D, 1>(p, job);
 }
 
-// The pieces of 32 rows joined: workgroup (row block x KV head, 32 dims), the pieces dealt to its four waves.
+// The pieces of 32 rows joined: workgroup (row block x KV head, kJoinDims dims), the pieces dealt to its four waves.
+constexpr int kJoinDims = 32;
 template <int DT, int D>
 __global__ __launch_bounds__(kCommonThreads) void common_join_kernel(const CommonParams p)
 {
     constexpr int kPieces = D / 8;
-    __shared__ float4 xo[kCommonWaves][4][64];
+    constexpr int J = kJoinDims / 8;
+    __shared__ float4 xo[kCommonWaves][J][64];
     __shared__ float2 xml[kCommonWaves][64];
     const int lane = threadIdx.x & 63, n32 = lane & 31, h2 = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int tile = p.by_kv_heads.div(blockIdx.x), g = blockIdx.x - tile * p.num_kv_heads, db = blockIdx.y;
+    const int tile = p.by_kv_heads.div(blockIdx.x), g = blockIdx.x - tile * p.num_kv_heads, part = blockIdx.y;
     const int r = 32 * tile + n32, rc = min(r, p.rows - 1), t = p.by_group.div(rc), head = g * p.group + (rc - t * p.group);
     const PlaceGuess guess(p, t);
     float m = -INFINITY, l = 0.f;
-    float4 acc[4];
+    float4 acc[J];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < J; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
     // kAtOnce pieces' loads in flight together.  at(i): piece i's number and the lane's row in it; i < n for the lane
     constexpr int kAtOnce = 4;
     auto join = [&](int n, int most, auto at) __attribute__((always_inline)) {
         for (int i0 = wave; i0 < most; i0 += kCommonWaves * kAtOnce) {
             float2 t2[kAtOnce];
-            float4 x[kAtOnce][4];
+            float4 x[kAtOnce][J];
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k) {
                 const int i = i0 + kCommonWaves * k;
                 t2[k] = make_float2(-INFINITY, 0.f);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x[k][j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int j = 0; j < J; ++j) x[k][j] = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (i < n) {
                     int row;
                     const int64_t piece = at(i, row);
                     t2[k] = p.ml[piece * 32 + row];
-                    const float4* const o = p.o + piece * (kPieces * 64) + 4 * db * 64 + row + 32 * h2;
+                    const float4* const o = p.o + piece * (kPieces * 64) + part * J * 64 + row + 32 * h2;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) x[k][j] = o[64 * j];
+                    for (int j = 0; j < J; ++j) x[k][j] = o[64 * j];
                 }
             }
             float m_new = m;
@@ -692,13 +703,13 @@ __global__ __launch_bounds__(kCommonThreads) void common_join_kernel(const Commo
             m = m_new;
             l *= f0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[j].x *= f0, acc[j].y *= f0, acc[j].z *= f0, acc[j].w *= f0;
+            for (int j = 0; j < J; ++j) acc[j].x *= f0, acc[j].y *= f0, acc[j].z *= f0, acc[j].w *= f0;
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k) {
                 const float f = t2[k].x == -INFINITY ? 0.f : fast_exp2(t2[k].x - m);
                 l = fmaf(f, t2[k].y, l);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < J; ++j) {
                     acc[j].x = fmaf(f, x[k][j].x, acc[j].x), acc[j].y = fmaf(f, x[k][j].y, acc[j].y);
                     acc[j].z = fmaf(f, x[k][j].z, acc[j].z), acc[j].w = fmaf(f, x[k][j].w, acc[j].w);
                 }
@@ -741,9 +752,10 @@ __global__ __launch_bounds__(kCommonThreads) void common_join_kernel(const Commo
     }
     xml[wave][lane] = make_float2(m, l);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) xo[wave][j][lane] = acc[j];
+    for (int j = 0; j < J; ++j) xo[wave][j][lane] = acc[j];
     __syncthreads();
-    // wave w: dims 8w + 4 h2 .. + 3 of the 32
+    if (wave >= J) return;
+    // wave w: dims 8w + 4 h2 .. + 3 of the workgroup's
     float m_all = -INFINITY, l_all = 0.f;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
@@ -762,7 +774,7 @@ __global__ __launch_bounds__(kCommonThreads) void common_join_kernel(const Commo
     uint2 packed;
     packed.x = l_all == 0.f ? 0u : narrow2<DT>(s.x * inv, s.y * inv);
     packed.y = l_all == 0.f ? 0u : narrow2<DT>(s.z * inv, s.w * inv);
-    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + ((int64_t)t * p.num_heads + head) * D + 32 * db + 8 * wave + 4 * h2) = packed;
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + ((int64_t)t * p.num_heads + head) * D + part * kJoinDims + 8 * wave + 4 * h2) = packed;
 }
 
 }  // namespace optgqa

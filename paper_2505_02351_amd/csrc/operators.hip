@@ -208,13 +208,13 @@ template <int DT, bool KV8, int D>
 int launch_common(const CommonParams& p, int workgroups, hipStream_t st)
 {
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&common_prefix_kernel<DT, KV8, D>),
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, kCommonLds<D>);
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, kCommonLds<D, KV8>);
     if (attr != hipSuccess) return OPTGQA_ERR_LAUNCH;
     if (workgroups > 0) {
-        const int rc = launch(common_prefix_kernel<DT, KV8, D>, dim3(workgroups), dim3(kCommonThreads), kCommonLds<D>, st, p);
+        const int rc = launch(common_prefix_kernel<DT, KV8, D>, dim3(workgroups), dim3(kCommonThreads), kCommonLds<D, KV8>, st, p);
         if (rc != OPTGQA_OK) return rc;
     }
-    return launch(common_join_kernel<DT, D>, dim3(p.p_slots * p.num_kv_heads, D / 32), dim3(kCommonThreads), 0, st, p);
+    return launch(common_join_kernel<DT, D>, dim3(p.p_slots * p.num_kv_heads, D / kJoinDims), dim3(kCommonThreads), 0, st, p);
 }
 
 template <int DT, bool KV8>

@@ -208,6 +208,25 @@ def test_what_a_row_does_not_see_does_not_reach_it(G, bad, dtype, D, rows):
     assert not torch.isfinite(out[last]).all(dim=1).any()
 
 
+@pytest.mark.parametrize("rows", [1, 3, 20])
+@pytest.mark.parametrize("dtype,D", [("f16", 64), ("bf16", 128), ("bf16", 64)])
+def test_codes_a_row_does_not_see_do_not_reach_it(G, dtype, D, rows):
+    """The same for E4M3 caches, whose only such code is NaN."""
+    import torch
+    n = 4 * rows
+    batch = Batch(13, dtype, 8, 1, D, 16, 3, [48 + 10 + n, 48 + 33], [n, 1], True, kv8=True).upload()
+    clean = batch.run(G)
+    batch.check(clean)
+    last = n - 2
+    for store in (batch.k, batch.v):
+        codes = store[0].view(torch.uint8)
+        codes[10 + last, :, ::5] = 0x7F
+        codes[10 + last + 1] = 0xFF
+    out = batch.upload().run(G)
+    assert torch.isfinite(out[:last]).all() and torch.equal(out[:last], clean[:last]) and torch.equal(out[n:], clean[n:])
+    assert not torch.isfinite(out[last]).all(dim=1).any()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_a_value_that_is_seen_is_not_lost(G, dtype):
     """An infinite value in a tile that some row's end cuts reaches the rows that see it, and no others."""
