@@ -377,7 +377,8 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
         if (__builtin_amdgcn_ballot_w64(first || mx > PfSoftmax<DT>::kThreshold) != 0) {
             mx = fmaxf(mx, __shfl_xor(mx, 32));                  // the row's keys live in 2 lanes (h2)
             const bool sees = mx > -INFINITY;
-            const float delta = first ? (sees ? mx + PfSoftmax<DT>::kHeadroom : 0.f) : fmaxf(mx + PfSoftmax<DT>::kHeadroom, 0.f);
+            // (0 for a row that did not ask: no row's bits depend on what its neighbours hold)
+            const float delta = (first ? sees : mx > PfSoftmax<DT>::kThreshold) ? mx + PfSoftmax<DT>::kHeadroom : 0.f;
             const float alpha = first ? 1.f : fast_exp2(-delta);
             started = started || sees;
             m_ref += delta;
@@ -552,7 +553,8 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
 
     // ---- what it leaves: the key groups' results joined, one piece for each row block ---------------------------
     const float l_row = lsum + __shfl_xor(lsum, 32);
-    const float m_row = started && row_ok ? m_ref : -INFINITY;
+    // (a row whose scores here are all NaN, a NaN query's, has no maximum; its sum says so, and has to reach the join)
+    const float m_row = row_ok && (started || l_row != l_row) ? m_ref : -INFINITY;
     float4* const o = p.o + (job.slot + rw) * (kPieces * 64) + lane;
     float2* const ml = p.ml + (job.slot + rw) * 32 + n32;
     auto piece_of = [&](int i) __attribute__((always_inline)) {

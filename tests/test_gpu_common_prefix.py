@@ -243,6 +243,30 @@ def test_a_value_that_is_seen_is_not_lost(G, dtype):
     assert dtype == "bf16" or (torch.isposinf(out[2:, :, 7]).all() and torch.isneginf(out[4:, :, 9]).all())
 
 
+@pytest.mark.parametrize("n", [1, 6, 20])        # one, two and four row blocks of 8-head groups
+@pytest.mark.parametrize("dtype,kv8,NP", [("f16", False, 3), ("bf16", False, 3), ("bf16", False, 0), ("bf16", True, 3)])
+def test_a_query_or_key_that_is_no_number_is_not_lost(G, dtype, kv8, NP, n):
+    """A NaN query's row, and the rows that see a NaN key, are NaN, also where no other key of a piece is seen; no others."""
+    import torch
+    P = 16 * NP
+    batch = Batch(14, dtype, 16, 2, 64, 16, NP, [P + n, P + 40], [n, 1], kv8=kv8).upload()
+    clean = batch.run(G)
+    batch.check(clean)
+    batch.q[n - 1, 3] = float("nan")
+    want = torch.zeros(clean.shape, dtype=torch.bool, device="cuda")
+    want[n - 1, 3] = True
+    out = batch.run(G)
+    assert torch.equal(torch.isnan(out), want) and torch.equal(out[~want], clean[~want])
+    # the first own key of sequence 0, second KV head: its only one behind the prefix where n is 1
+    if kv8:
+        batch.k[0].view(torch.uint8)[0, 1, 5] = 0x7F
+    else:
+        batch.k[0][0, 1, 5] = float("nan")
+    want[:n, 8:] = True
+    out = batch.upload().run(G)
+    assert torch.equal(torch.isnan(out), want) and torch.equal(out[~want], clean[~want])
+
+
 def test_loud_scores_and_zero_scale(G):
     for scale in (0.0, -0.05, 3.0):
         batch = Batch(7, "f16", 8, 2, 64, 16, 9, [200, 170, 144], [1, 2, 1]).upload()
