@@ -89,7 +89,7 @@ def _rows(t: torch.Tensor, name: str, tokens: int, D: int) -> Tuple[int, int]:
     if len(shape) != 3 or shape[0] != tokens or shape[2] != D:
         raise ValueError(f"optgqa: {name} must be [{tokens}, heads, {D}], got {tuple(shape)}")
     H, stride = shape[1], t.stride()
-    if tokens > 1 and H and (stride[2] != 1 or (H > 1 and stride[1] != D)) or tokens == 1 and H > 1 and (stride[2] != 1 or stride[1] != D):
+    if tokens and H and (stride[2] != 1 or (H > 1 and stride[1] != D)):
         raise ValueError(f"optgqa: {name} must be dense in its last two dims")
     return H, stride[0] if tokens > 1 else H * D
 

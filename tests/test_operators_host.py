@@ -110,6 +110,17 @@ def test_the_binding_refuses_what_the_library_cannot_see(G):
         G.rotary_embedding(q, q, k, k, pos, f)                   # not on a GPU
 
 
+def test_rows_that_are_not_dense_are_refused(G):
+    import torch
+    from paper_2505_02351_amd.operators import _rows
+    assert _rows(torch.zeros(3, 2, 64), "q", 3, 64) == (2, 128) and _rows(torch.zeros(3, 200)[:, 8:136].view(3, 2, 64), "q", 3, 64) == (2, 200)
+    assert _rows(torch.zeros(5, 64, 1, dtype=torch.float16).transpose(1, 2)[:1], "q", 1, 64) == (1, 64)
+    for T, H in ((1, 1), (1, 2), (3, 1), (3, 2)):
+        for t in (torch.zeros(T, H, 128)[:, :, ::2], torch.zeros(T, 64, max(H, 2)).transpose(1, 2)[:, :H]):
+            with pytest.raises(ValueError):
+                _rows(t, "q", T, 64)
+
+
 def test_verification_refuses_before_any_launch(G):
     lib = G.load_library()
     need = G.verify_drafts_workspace_bytes(3, 32000)
