@@ -590,6 +590,7 @@ int optgqa_rotary_frequencies_host(double *freqs_host, float *magnitude_host, in
  *   prefix_table    [num_prefix_blocks] int32, full blocks; num_prefix_blocks may be 0
  *   cu_q_lens       [num_seqs + 1] int32 prefix sums, or NULL: one new token each (num_tokens == num_seqs)
  *   max_context_len, max_q_len   upper bounds on the context lengths (prefix included) and the n_b; they size the launch
+ *                   (OPTGQA_ERR_SHAPE beyond 2^30 tokens, 2^25 behind the prefix)
  *   workspace       optgqa_common_prefix_workspace_bytes(...) bytes, 16-byte aligned (OPTGQA_ERR_WORKSPACE without it)
  * The 8-bit calls run over E4M3 caches, scales as for optgqa_paged_attention_fp8 and _fp8_heads.  Other arguments and errors as
  * optgqa_paged_attention.  Infinities and NaN in

@@ -193,8 +193,10 @@ bool plan_common(CommonPlan& c, int64_t num_tokens, int64_t num_seqs, int num_he
     c.s_row_waves = common_row_waves(own_rows);
     if (behind > 0) {
         const int64_t tile_rows = 32 * c.s_row_waves, step = 32 * (kCommonWaves / c.s_row_waves);
-        const int64_t steps = num_seqs * num_kv_heads * ((own_rows + tile_rows - 1) / tile_rows) * ((behind + step - 1) / step);
-        if (steps >= (1ll << 30)) return false;
+        // row tiles: of all sequences at the bound, or of all tokens and one begun by each sequence
+        const int64_t tiles = std::min(num_seqs * ((own_rows + tile_rows - 1) / tile_rows), c.rows / tile_rows + num_seqs);
+        const int64_t each = (behind + step - 1) / step, steps = num_kv_heads * tiles * each;
+        if (each > (1 << 20) || steps >= (1ll << 30)) return false;
         // (a piece of half of all CUs' share: with more pieces, and with fewer, 64 sequences behind 4 096 tokens, own parts of 127 - 1 023, take
         // 37 - 38 us instead of 32, behind 32 768, 1 023 - 2 047, 110 - 125 instead of 110)
         c.s_shares = (int)std::min<int64_t>(std::max<int64_t>(cus / 2, 1), steps);

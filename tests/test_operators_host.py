@@ -180,6 +180,15 @@ def test_common_prefix_workspace_covers_every_smaller_call(G):
         assert big >= G.common_prefix_workspace_bytes(T, B, Hq, Hkv, D, 16, NP, Lmax, 1)
 
 
+def test_common_prefix_sizes_at_their_ends(G):
+    """Chunks of long contexts fit where the bound on one sequence's tokens, taken for all of them, would not."""
+    def need(T, B, Lmax, n, Hq=64, Hkv=8):
+        return G.common_prefix_workspace_bytes(T, B, Hq, Hkv, 128, 16, 0, Lmax, n)
+    assert need(8192 + 63, 64, 1 << 20, 8192) > 0
+    assert need(1, 1, 1 << 25, 1) > 0 and need(1, 1, (1 << 25) + 1, 1, 128, 1) == 0
+    assert need(128, 1, 1 << 25, 128, 1, 1) > 0 and need(128, 1, (1 << 25) + 1, 128, 1, 1) == 0
+
+
 def test_types_are_refused_before_places(G):
     """CPU tensors throughout: a wrong type is a TypeError, right types a ValueError."""
     import torch
