@@ -659,13 +659,62 @@ __global__ __launch_bounds__(kCommonThreads, 2) void common_prefix_kernel(const 
     else common_body<DT, KV8, D, 1>(p, job);
 }
 
-// The pieces of 32 rows joined: workgroup (row block x KV head, kJoinDims dims), the pieces dealt to its four waves.
-constexpr int kJoinDims = 32;
-template <int DT, int D>
+// N pieces of a lane's row: i0, i0 + 4, ..; of 8 J of their dims the lane's halves.
+template <int D, int J, int N> struct JoinBatch {
+    static constexpr int kPieceVectors = D / 8 * 64;
+    float2 ml[N];
+    float4 x[N][J];
+    // at(i, row): number of piece i, and how far the row in it lies from row n32; those below n are there
+    template <typename At>
+    __device__ __forceinline__ void load(const CommonParams& p, const float4* o, int n32, int i0, int n, At at)
+    {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int i = i0 + kCommonWaves * k;
+            ml[k] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (int j = 0; j < J; ++j) x[k][j] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (i < n) {
+                int row;
+                const int64_t piece = at(i, row);
+                ml[k] = p.ml[piece * 32 + n32 + row];
+                const float4* const from = o + piece * kPieceVectors + row;
+#pragma unroll
+                for (int j = 0; j < J; ++j) x[k][j] = from[64 * j];
+            }
+        }
+    }
+};
+template <int J> struct JoinState {
+    float m = -INFINITY, l = 0.f;
+    float4 acc[J] = {};
+    template <int D, int N> __device__ __forceinline__ void add(const JoinBatch<D, J, N>& b)
+    {
+        float m_new = m;
+#pragma unroll
+        for (int k = 0; k < N; ++k) m_new = fmaxf(m_new, b.ml[k].x);
+        const float f0 = m == -INFINITY ? 0.f : fast_exp2(m - m_new);
+        m = m_new;
+        l *= f0;
+#pragma unroll
+        for (int j = 0; j < J; ++j) acc[j].x *= f0, acc[j].y *= f0, acc[j].z *= f0, acc[j].w *= f0;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float f = b.ml[k].x == -INFINITY ? 0.f : fast_exp2(b.ml[k].x - m);
+            l = fmaf(f, b.ml[k].y, l);
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                acc[j].x = fmaf(f, b.x[k][j].x, acc[j].x), acc[j].y = fmaf(f, b.x[k][j].y, acc[j].y);
+                acc[j].z = fmaf(f, b.x[k][j].z, acc[j].z), acc[j].w = fmaf(f, b.x[k][j].w, acc[j].w);
+            }
+        }
+    }
+};
+// The pieces of 32 rows joined: workgroup (row block x KV head, DIMS dims), the pieces dealt to its four waves.
+template <int DT, int D, int DIMS>
 __global__ __launch_bounds__(kCommonThreads) void common_join_kernel(const CommonParams p)
 {
-    constexpr int kPieces = D / 8;
-    constexpr int J = kJoinDims / 8;
+    constexpr int J = DIMS / 8;
     __shared__ float4 xo[kCommonWaves][J][64];
     __shared__ float2 xml[kCommonWaves][64];
     const int lane = threadIdx.x & 63, n32 = lane & 31, h2 = lane >> 5;
@@ -673,64 +722,25 @@ __global__ __launch_bounds__(kCommonThreads) void common_join_kernel(const Commo
     const int tile = p.by_kv_heads.div(blockIdx.x), g = blockIdx.x - tile * p.num_kv_heads, part = blockIdx.y;
     const int r = 32 * tile + n32, rc = min(r, p.rows - 1), t = p.by_group.div(rc), head = g * p.group + (rc - t * p.group);
     const PlaceGuess guess(p, t);
-    float m = -INFINITY, l = 0.f;
-    float4 acc[J];
-#pragma unroll
-    for (int i = 0; i < J; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    // kAtOnce pieces' loads in flight together.  at(i): piece i's number and the lane's row in it; i < n for the lane
-    constexpr int kAtOnce = 4;
-    auto join = [&](int n, int most, auto at) __attribute__((always_inline)) {
-        for (int i0 = wave; i0 < most; i0 += kCommonWaves * kAtOnce) {
-            float2 t2[kAtOnce];
-            float4 x[kAtOnce][J];
-#pragma unroll
-            for (int k = 0; k < kAtOnce; ++k) {
-                const int i = i0 + kCommonWaves * k;
-                t2[k] = make_float2(-INFINITY, 0.f);
-#pragma unroll
-                for (int j = 0; j < J; ++j) x[k][j] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (i < n) {
-                    int row;
-                    const int64_t piece = at(i, row);
-                    t2[k] = p.ml[piece * 32 + row];
-                    const float4* const o = p.o + piece * (kPieces * 64) + part * J * 64 + row + 32 * h2;
-#pragma unroll
-                    for (int j = 0; j < J; ++j) x[k][j] = o[64 * j];
-                }
-            }
-            float m_new = m;
-#pragma unroll
-            for (int k = 0; k < kAtOnce; ++k) m_new = fmaxf(m_new, t2[k].x);
-            const float f0 = m == -INFINITY ? 0.f : fast_exp2(m - m_new);
-            m = m_new;
-            l *= f0;
-#pragma unroll
-            for (int j = 0; j < J; ++j) acc[j].x *= f0, acc[j].y *= f0, acc[j].z *= f0, acc[j].w *= f0;
-#pragma unroll
-            for (int k = 0; k < kAtOnce; ++k) {
-                const float f = t2[k].x == -INFINITY ? 0.f : fast_exp2(t2[k].x - m);
-                l = fmaf(f, t2[k].y, l);
-#pragma unroll
-                for (int j = 0; j < J; ++j) {
-                    acc[j].x = fmaf(f, x[k][j].x, acc[j].x), acc[j].y = fmaf(f, x[k][j].y, acc[j].y);
-                    acc[j].z = fmaf(f, x[k][j].z, acc[j].z), acc[j].w = fmaf(f, x[k][j].w, acc[j].w);
-                }
-            }
-        }
-    };
-    // the prefix's pieces are there for every row, whatever it sees (m = -inf: nothing)
-    join(p.p_splits, p.p_splits, [&](int i, int& row) __attribute__((always_inline)) {
-        row = n32;
+    OwnParts parts(p, 0);
+    JoinState<J> state;
+    const float4* const o = p.o + part * J * 64 + n32 + 32 * h2;
+    // the prefix's pieces are there for every row, whatever it sees (m = -inf: nothing): those of a wave, four at a time, the
+    // first ones under way while it is found out which are the row's own
+    JoinBatch<D, J, 4> prefix;
+    auto prefix_at = [&](int i, int& row) __attribute__((always_inline)) {
+        row = 0;
         return ((int64_t)i * p.num_kv_heads + g) * p.p_slots + tile;
-    });
+    };
+    prefix.load(p, o, n32, wave, p.p_splits, prefix_at);
     // its own: the steps in which it sees a key, and the workgroups that had them
+    int n = 0, row_off = 0;
+    int64_t piece0 = 0;
     if (p.s_shares > 0) {
         const TokenPlace at = guess.find(p, t);
         const int behind = at.pos(t) + 1 - p.prefix_len;
-        OwnParts parts(p, 0);
         const int share = own_share(p, parts);
-        int n = 0, row_in_tile = 0, all = 0;
-        int64_t piece0 = 0;
+        int all = 0;
         for (int from = 0;;) {
             parts.number(share, all);
             const int l = at.seq - from;                         // (all lanes exchange)
@@ -740,18 +750,32 @@ __global__ __launch_bounds__(kCommonThreads) void common_join_kernel(const Commo
                 const int tiles = ((at.end - at.first) * p.group + tile_rows - 1) >> tile_shift;
                 const int each = OwnParts::each(steps, pieces);
                 n = div_by_inverse(OwnParts::steps_of(p, behind) + each - 1, each, __builtin_amdgcn_rcpf((float)each));
-                row_in_tile = in_seq & 31;
+                row_off = (in_seq & 31) - n32;
                 piece0 = p.s_first + (int64_t)(before + (g * tiles + (in_seq >> tile_shift)) * pieces) * p.s_row_waves + ((in_seq >> 5) & (p.s_row_waves - 1));
             }
             from += 64;
             if (from >= p.num_seqs) break;
             parts = OwnParts(p, from);
         }
-        join(n, wave_max(n), [&](int i, int& row) __attribute__((always_inline)) {
-            row = row_in_tile;
-            return piece0 + (int64_t)i * p.s_row_waves;
-        });
     }
+    auto own_at = [&](int i, int& row) __attribute__((always_inline)) {
+        row = row_off;
+        return piece0 + (int64_t)i * p.s_row_waves;
+    };
+    JoinBatch<D, J, 2> own;
+    own.load(p, o, n32, wave, n, own_at);
+    state.add(prefix);
+    for (int i0 = wave + 4 * kCommonWaves; i0 < p.p_splits; i0 += 4 * kCommonWaves) {
+        prefix.load(p, o, n32, i0, p.p_splits, prefix_at);
+        state.add(prefix);
+    }
+    state.add(own);
+    for (int i0 = wave + 2 * kCommonWaves, most = wave_max(n); i0 < most; i0 += 2 * kCommonWaves) {
+        own.load(p, o, n32, i0, n, own_at);
+        state.add(own);
+    }
+    const float m = state.m, l = state.l;
+    const auto& acc = state.acc;
     xml[wave][lane] = make_float2(m, l);
 #pragma unroll
     for (int j = 0; j < J; ++j) xo[wave][j][lane] = acc[j];
@@ -776,7 +800,7 @@ __global__ __launch_bounds__(kCommonThreads) void common_join_kernel(const Commo
     uint2 packed;
     packed.x = l_all == 0.f ? 0u : narrow2<DT>(s.x * inv, s.y * inv);
     packed.y = l_all == 0.f ? 0u : narrow2<DT>(s.z * inv, s.w * inv);
-    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + ((int64_t)t * p.num_heads + head) * D + part * kJoinDims + 8 * wave + 4 * h2) = packed;
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + ((int64_t)t * p.num_heads + head) * D + part * DIMS + 8 * wave + 4 * h2) = packed;
 }
 
 }  // namespace optgqa

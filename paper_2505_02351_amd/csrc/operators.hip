@@ -216,7 +216,11 @@ int launch_common(const CommonParams& p, int workgroups, hipStream_t st)
         const int rc = launch(common_prefix_kernel<DT, KV8, D>, dim3(workgroups), dim3(kCommonThreads), kCommonLds<D, KV8>, st, p);
         if (rc != OPTGQA_OK) return rc;
     }
-    return launch(common_join_kernel<DT, D>, dim3(p.p_slots * p.num_kv_heads, D / kJoinDims), dim3(kCommonThreads), 0, st, p);
+    // 32 dims to a workgroup of the join, 16 where those would not be one to a CU (16 sequences of 32 / 8 heads of 128 behind 6 528
+    // tokens: 16.0 us against 16.4; 32 of 3 - 6 new tokens each, 40 / 8 heads: 47.1 against 44.9)
+    const int tiles = p.p_slots * p.num_kv_heads;
+    return (int64_t)tiles * (D / 32) < num_cus() ? launch(common_join_kernel<DT, D, 16>, dim3(tiles, D / 16), dim3(kCommonThreads), 0, st, p)
+                                                 : launch(common_join_kernel<DT, D, 32>, dim3(tiles, D / 32), dim3(kCommonThreads), 0, st, p);
 }
 
 template <int DT, bool KV8>
