@@ -10,6 +10,7 @@
 // flight at once; they leave their sums.  In a second launch a wave for each sequence looks up the chunk that the draw falls in and reads
 // that one again.  What is left is latency: three dependent round trips to memory to judge the drafts, one for the row, then two in the second
 // launch.
+// Measured: 64 sequences of 128 255 entries, fp32: 17.7 us (kernels 14.1, 4.7 TB/s, and 4.2); one of 32 000: 11.0 (4.2 + 3.8, the rest is the calls).
 #pragma once
 #include "common.hpp"
 
