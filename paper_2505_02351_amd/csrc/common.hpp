@@ -148,6 +148,28 @@ __device__ __forceinline__ int wave_max(int x)
                max(__builtin_amdgcn_readlane(x, 32), __builtin_amdgcn_readlane(x, 48)));
 }
 
+// Inclusive sums over the lanes, without a trip through LDS: within rows of 16, then each odd row with the end of the row before
+// it, then the upper half with the end of the lower one.
+constexpr int kDppRowShr1 = 0x111, kDppRowShr2 = 0x112, kDppRowShr4 = 0x114, kDppRowShr8 = 0x118;
+constexpr int kDppRowBcast15 = 0x142, kDppRowBcast31 = 0x143;
+template <int CTRL, int ROWS> __device__ __forceinline__ int dpp_or_0(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false); }
+template <int CTRL, int ROWS> __device__ __forceinline__ double dpp_or_0(double x)
+{
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = (uint32_t)dpp_or_0<CTRL, ROWS>((int)(uint32_t)u), hi = (uint32_t)dpp_or_0<CTRL, ROWS>((int)(uint32_t)(u >> 32));
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <typename T> __device__ __forceinline__ T lane_sums(T x)
+{
+    x += dpp_or_0<kDppRowShr1, 0xf>(x);
+    x += dpp_or_0<kDppRowShr2, 0xf>(x);
+    x += dpp_or_0<kDppRowShr4, 0xf>(x);
+    x += dpp_or_0<kDppRowShr8, 0xf>(x);
+    x += dpp_or_0<kDppRowBcast15, 0xa>(x);
+    x += dpp_or_0<kDppRowBcast31, 0xc>(x);
+    return x;
+}
+
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Softmax references that are moved lazily (decode_mc_kernels.hpp):

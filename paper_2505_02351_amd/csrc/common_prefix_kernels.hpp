@@ -121,18 +121,6 @@ struct PlaceGuess {
     }
 };
 
-// inclusive sum over the lanes
-__device__ __forceinline__ int lane_sums(int x)
-{
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const int y = __shfl_up(x, off);
-        x += lane >= off ? y : 0;
-    }
-    return x;
-}
-
 // Own parts of 64 sequences, one a lane.  A segment: one KV head, one row tile.
 struct OwnParts {
     int len, first, rows;       // context length, first token, rows (new tokens x heads of the group)

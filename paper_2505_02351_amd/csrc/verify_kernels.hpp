@@ -10,7 +10,7 @@
 // flight at once; they leave their sums.  In a second launch a wave for each sequence looks up the chunk that the draw falls in and reads
 // that one again.  What is left is latency: three dependent round trips to memory to judge the drafts, one for the row, then two in the second
 // launch.
-// Measured: 64 sequences of 128 255 entries, fp32: 17.7 us (kernels 14.1, 4.7 TB/s, and 4.2); one of 32 000: 11.0 (4.2 + 3.8, the rest is the calls).
+// Measured: 64 sequences of 128 255 entries, fp32: 17.0 us (kernels 13.5, 4.9 TB/s, and 3.9); one of 32 000: 11.2 (4.1 + 3.1, the rest is the calls).
 #pragma once
 #include "common.hpp"
 
@@ -145,13 +145,6 @@ __device__ __forceinline__ void entries(const VerifyParams& a, const unsigned ch
     }
 }
 
-__device__ __forceinline__ double wave_sum(double x)
-{
-#pragma unroll
-    for (int off = 32; off; off >>= 1) x += __shfl_xor(x, off);
-    return x;
-}
-
 // Sums of sequence blockIdx.x's rows, a chunk to a wave.
 template <int DT>
 __global__ __launch_bounds__(kVerifyThreads) void verify_sums_kernel(const VerifyParams a)
@@ -168,23 +161,11 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_sums_kernel(const Verif
     double l = 0.0, p = 0.0;
 #pragma unroll
     for (int i = 0; i < kVerifyEach; ++i) l += left[i], p += all[i];
-    l = wave_sum(l), p = wave_sum(p);
-    if (lane == 0) {
+    l = lane_sums(l), p = lane_sums(p);
+    if (lane == 63) {
         a.sums[(int64_t)b * a.chunks + chunk] = make_double2(l, p);
         if (chunk == 0) a.verdicts[b] = v;
     }
-}
-
-// inclusive sum over the lanes
-__device__ __forceinline__ double lane_sums(double x)
-{
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const double y = __shfl_up(x, off);
-        x += lane >= off ? y : 0.0;
-    }
-    return x;
 }
 
 // The draw of sequence blockIdx.x, and its row of tokens.  Where rounding lets no sum pass the bar, the last entry that counts is drawn.
