@@ -149,6 +149,8 @@ int rotary_and_cache_impl(void* q_out, const void* q, const void* k, const void*
 template <int DT>
 int launch_verify(const VerifyParams& a, int num_seqs, hipStream_t st)
 {
+    if (a.chunks <= kVerifyOneChunks)
+        return launch(verify_one_kernel<DT>, dim3(num_seqs), dim3(64 * kVerifyOneWaves), 0, st, a);
     constexpr int kWaves = kVerifyThreads / 64;
     const int rc = launch(verify_sums_kernel<DT>, dim3(num_seqs, (a.chunks + kWaves - 1) / kWaves), dim3(kVerifyThreads), 0, st, a);
     return rc != OPTGQA_OK ? rc : launch(verify_select_kernel<DT>, dim3(num_seqs), dim3(64), 0, st, a);

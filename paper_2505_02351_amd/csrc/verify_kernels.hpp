@@ -8,9 +8,9 @@
 // Bound by memory: one row of p and one of q per sequence, everything else is a few scattered entries.  Rows are long
 // (10^4 to 10^5 entries) and sequences few, so a row is cut into chunks of 1 024 entries, a wave each, with all its loads in
 // flight at once; they leave their sums.  In a second launch a wave for each sequence looks up the chunk that the draw falls in and reads
-// that one again.  What is left is latency: three dependent round trips to memory to judge the drafts, one for the row, then two in the second
+// that one again; rows of up to 32 chunks have both in one.  What is left is latency: three dependent round trips to memory to judge the drafts, one for the row, then two in the second
 // launch.
-// Measured: 64 sequences of 128 255 entries, fp32: 17.0 us (kernels 13.5, 4.9 TB/s, and 3.9); one of 32 000: 11.2 (4.1 + 3.1, the rest is the calls).
+// Measured: 64 sequences of 128 255 entries, fp32: 17.5 us (kernels 13.2, 5.0 TB/s, and 4.5); one of 32 000: 8.7, the call.
 #pragma once
 #include "common.hpp"
 
@@ -145,15 +145,9 @@ __device__ __forceinline__ void entries(const VerifyParams& a, const unsigned ch
     }
 }
 
-// Sums of sequence blockIdx.x's rows, a chunk to a wave.
-template <int DT>
-__global__ __launch_bounds__(kVerifyThreads) void verify_sums_kernel(const VerifyParams a)
+// Sums of a chunk of the entries to draw from and of p, in lane 63.
+template <int DT> __device__ __forceinline__ double2 chunk_sums(const VerifyParams& a, int b, int c0, const Verdict& v, int chunk)
 {
-    const int b = blockIdx.x, lane = threadIdx.x & 63;
-    const int chunk = blockIdx.y * (kVerifyThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (chunk >= a.chunks) return;
-    const int c0 = a.cu[b], count = min(max(a.cu[b + 1] - c0, 0), a.looked_at);
-    const Verdict v = judge_drafts<DT>(a, b, c0, count);
     constexpr int ES = kProbabilityBytes<DT>;
     double left[kVerifyEach], all[kVerifyEach];
     entries<DT, false>(a, target_rows<DT>(a, b, c0) + v.kept * a.target_stride * ES, v.minus ? draft_rows<DT>(a, c0) + v.kept * a.draft_stride * ES : nullptr,
@@ -161,22 +155,15 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_sums_kernel(const Verif
     double l = 0.0, p = 0.0;
 #pragma unroll
     for (int i = 0; i < kVerifyEach; ++i) l += left[i], p += all[i];
-    l = lane_sums(l), p = lane_sums(p);
-    if (lane == 63) {
-        a.sums[(int64_t)b * a.chunks + chunk] = make_double2(l, p);
-        if (chunk == 0) a.verdicts[b] = v;
-    }
+    return make_double2(lane_sums(l), lane_sums(p));
 }
 
-// The draw of sequence blockIdx.x, and its row of tokens.  Where rounding lets no sum pass the bar, the last entry that counts is drawn.
-template <int DT>
-__global__ __launch_bounds__(64) void verify_select_kernel(const VerifyParams a)
+// The draw of sequence b by one wave, from the sums of its chunks, and its row of tokens.  Where rounding lets no sum pass the bar, the last
+// entry that counts is drawn.
+template <int DT> __device__ __forceinline__ void select_token(const VerifyParams& a, int b, int c0, const Verdict& v, const double2* sums)
 {
     constexpr int ES = kProbabilityBytes<DT>;
-    const int b = blockIdx.x, lane = threadIdx.x;
-    const double2* const sums = a.sums + (int64_t)b * a.chunks;
-    const int c0 = a.cu[b];
-    const Verdict v = a.verdicts[b];
+    const int lane = threadIdx.x & 63;
     const double u = a.sample_u[b];
     // a lane has `each` consecutive chunks
     const int each = (a.chunks + 63) / 64, first = lane * each, end = min(first + each, a.chunks);
@@ -227,6 +214,50 @@ __global__ __launch_bounds__(64) void verify_select_kernel(const VerifyParams a)
     if (lane == 0) a.accepted[b] = v.kept;
     for (int i = lane; i <= a.max_drafts; i += 64)
         a.tokens[(int64_t)b * (a.max_drafts + 1) + i] = i < v.kept ? a.draft_tokens[(int64_t)c0 + i] : i == v.kept ? token : -1;
+}
+
+// Sums of sequence blockIdx.x's rows, a chunk to a wave.
+template <int DT>
+__global__ __launch_bounds__(kVerifyThreads) void verify_sums_kernel(const VerifyParams a)
+{
+    const int b = blockIdx.x, lane = threadIdx.x & 63;
+    const int chunk = blockIdx.y * (kVerifyThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (chunk >= a.chunks) return;
+    const int c0 = a.cu[b], count = min(max(a.cu[b + 1] - c0, 0), a.looked_at);
+    const Verdict v = judge_drafts<DT>(a, b, c0, count);
+    const double2 s = chunk_sums<DT>(a, b, c0, v, chunk);
+    if (lane == 63) {
+        a.sums[(int64_t)b * a.chunks + chunk] = s;
+        if (chunk == 0) a.verdicts[b] = v;
+    }
+}
+
+// The draw of sequence blockIdx.x.
+template <int DT>
+__global__ __launch_bounds__(64) void verify_select_kernel(const VerifyParams a)
+{
+    const int b = blockIdx.x;
+    select_token<DT>(a, b, a.cu[b], a.verdicts[b], a.sums + (int64_t)b * a.chunks);
+}
+
+// Both in one launch, for rows of up to two chunks to each of a workgroup's sixteen waves.  Us a call, and of GPU time, two launches against
+// one, fp32: one sequence of 4 096 entries 10.7 -> 8.5 and 6.6 -> 5.4, of 32 000 10.6 -> 8.7 and 7.2 -> 8.7 (the second chunk's loads wait
+// for the first's; more of them under way in straight code: 9.0, that code has to be fetched), 64 of 16 000 10.6 -> 8.4 and 8.5 -> 7.8, 256
+// of 32 000 17.5 -> 14.3 and 17.7 -> 14.4.
+constexpr int kVerifyOneWaves = 16, kVerifyOneChunks = 2 * kVerifyOneWaves;
+template <int DT>
+__global__ __launch_bounds__(64 * kVerifyOneWaves) void verify_one_kernel(const VerifyParams a)
+{
+    __shared__ double2 sums[kVerifyOneChunks];
+    const int b = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c0 = a.cu[b], count = min(max(a.cu[b + 1] - c0, 0), a.looked_at);
+    const Verdict v = judge_drafts<DT>(a, b, c0, count);
+    for (int chunk = wave; chunk < a.chunks; chunk += kVerifyOneWaves) {
+        const double2 s = chunk_sums<DT>(a, b, c0, v, chunk);
+        if (lane == 63) sums[chunk] = s;
+    }
+    __syncthreads();
+    if (wave == 0) select_token<DT>(a, b, c0, v, sums);
 }
 
 }  // namespace optgqa

@@ -67,6 +67,20 @@ def test_random_drafts(G, V, pad, sampled, dtype):
         assert (want[0][np.arange(B), want[1]] >= 0).all()
 
 
+@pytest.mark.parametrize("sampled", [True, False])
+@pytest.mark.parametrize("V", [1023, 1024, 1025, 16384, 16385, 32767, 32768, 32769, 33793])
+def test_draws_from_every_chunk(G, V, sampled):
+    """Vocabularies around a chunk of 1 024, a wave's of 16 and the 32 that one launch takes; draws spread over the whole row."""
+    import torch
+    counts = [i % 3 for i in range(67)]
+    target, draft, ids, a, s = inputs(V, counts, V, torch.float32, sampled)
+    s[:] = np.linspace(0.0, 0.9999, len(s), dtype=np.float32)
+    want = check(G, target, draft, ids, counts, a, s, 3)
+    drawn = want[0][np.arange(67), want[1]]
+    # (what the oracle drew: most chunks)
+    assert (drawn >= 0).all() and 2 * np.unique(drawn // 1024).size >= min(-(-V // 1024), 32)
+
+
 def test_many_drafts_and_many_sequences(G):
     """More drafts than a wave has lanes, and more than max_drafts; hundreds of sequences; a vocabulary of many chunks."""
     import torch
