@@ -161,6 +161,14 @@ __device__ __forceinline__ int own_share(const CommonParams& p, const OwnParts& 
     return max(p.by_s_shares.div(total + p.s_shares - 1), 1);
 }
 
+// How far a tile's maximum may lie above a row's reference, and where the reference is put when one does (log2 units above that
+// maximum).  bf16: as everywhere.  fp16 weights are rounded once, and a range may be a whole long prefix whose many small
+// weights add up beside one large one: the reference lies below the maximum, so that weights down to 24 binary orders under the largest are
+// normal numbers and those down to 35 are there (2 above it, as in the prefill kernel: 12 and 23; 32 767 keys 21.25 orders under one
+// key came to 1.54e-2 in place of 1.30e-2).  The room up to 2^15 is what keeps rescales few: maxima that grow by less than 5 orders need none.
+template <int DT> struct CommonSoftmax { static constexpr float kThreshold = PfSoftmax<DT>::kThreshold, kHeadroom = PfSoftmax<DT>::kHeadroom; };
+template <> struct CommonSoftmax<kF16> { static constexpr float kThreshold = 15.f, kHeadroom = -10.f; };
+
 // A workgroup's rows and keys.
 struct CommonJob {
     bool prefix;
@@ -367,11 +375,11 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
 #pragma unroll
         for (int e = 1; e < 16; ++e) mx = fmaxf(mx, x[e]);
         const bool first = !started;
-        if (__builtin_amdgcn_ballot_w64(first || mx > PfSoftmax<DT>::kThreshold) != 0) {
+        if (__builtin_amdgcn_ballot_w64(first || mx > CommonSoftmax<DT>::kThreshold) != 0) {
             mx = fmaxf(mx, __shfl_xor(mx, 32));                  // the row's keys live in 2 lanes (h2)
             const bool sees = mx > -INFINITY;
             // (0 for a row that did not ask: no row's bits depend on what its neighbours hold)
-            const float delta = (first ? sees : mx > PfSoftmax<DT>::kThreshold) ? mx + PfSoftmax<DT>::kHeadroom : 0.f;
+            const float delta = (first ? sees : mx > CommonSoftmax<DT>::kThreshold) ? mx + CommonSoftmax<DT>::kHeadroom : 0.f;
             const float alpha = first ? 1.f : fast_exp2(-delta);
             started = started || sees;
             m_ref += delta;
