@@ -62,8 +62,9 @@ class Server:
         shape = (blocks.shape[0], model.kv_heads, block, model.dim)
         self.caches = [[torch.zeros(shape, dtype=model.dtype, device="cuda") for _ in "kv"] for _ in model.qkv]
         self.max_len, self.scale = self.prefix_len + max_tokens + drafts + 1, 1.0 / math.sqrt(model.dim)
-        self.ws = torch.empty(max(G.common_prefix_workspace_bytes(T, sequences, model.heads, model.kv_heads, model.dim, block, NP, self.max_len, n)
-                                  for T, n in ((sequences, 1), (sequences * (drafts + 1), drafts + 1))), dtype=torch.uint8, device="cuda")
+        # (drafts are the most that a step has: steps of one token fit, too)
+        self.ws = torch.empty(G.common_prefix_workspace_bytes(sequences * (drafts + 1), sequences, model.heads, model.kv_heads, model.dim, block, NP,
+                                                              self.max_len, drafts + 1), dtype=torch.uint8, device="cuda")
         self.verify_ws = torch.empty(G.verify_drafts_workspace_bytes(sequences, model.vocab), dtype=torch.uint8, device="cuda")
         self._prefill(prompt)
 

@@ -591,7 +591,9 @@ int optgqa_rotary_frequencies_host(double *freqs_host, float *magnitude_host, in
  *   cu_q_lens       [num_seqs + 1] int32 prefix sums, or NULL: one new token each (num_tokens == num_seqs)
  *   max_context_len, max_q_len   upper bounds on the context lengths (prefix included) and the n_b; they size the launch
  *                   (OPTGQA_ERR_SHAPE beyond 2^30 tokens, 2^25 behind the prefix)
- *   workspace       optgqa_common_prefix_workspace_bytes(...) bytes, 16-byte aligned (OPTGQA_ERR_WORKSPACE without it)
+ *   workspace       optgqa_common_prefix_workspace_bytes(...) bytes, 16-byte aligned (OPTGQA_ERR_WORKSPACE without it).  The size
+ *                   grows with every one of num_tokens, num_seqs, num_prefix_blocks, max_context_len and max_q_len: a
+ *                   workspace for the largest of each serves every call
  * The 8-bit calls run over E4M3 caches, scales as for optgqa_paged_attention_fp8 and _fp8_heads.  Other arguments and errors as
  * optgqa_paged_attention.  Infinities and NaN in
  * keys and values that a row does not see do not reach it; an infinite value that it sees makes that element of it no

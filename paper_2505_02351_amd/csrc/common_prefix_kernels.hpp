@@ -25,11 +25,10 @@
 #pragma once
 #include <type_traits>
 
+#include "common_prefix_shape.hpp"
 #include "mfma_tiles.hpp"
 
 namespace optgqa {
-
-constexpr int kCommonThreads = 256, kCommonWaves = 4;
 
 // A tile of 32 keys in LDS, as the memory system writes it (see PfDirect): 2-byte rows, or 8-bit codes as they are.  Rows of as many
 // bytes lie alike; the 64 bytes of a row of 64 codes, 16 rows to a group, with their columns of 16 bytes exchanged by

@@ -9,6 +9,7 @@
 #include <cmath>
 
 #include "common_prefix_kernels.hpp"
+#include "common_prefix_shape.hpp"
 #include "host.hpp"
 #include "rotary_kernels.hpp"
 #include "verify_kernels.hpp"
@@ -156,58 +157,6 @@ int launch_verify(const VerifyParams& a, int num_seqs, hipStream_t st)
     return rc != OPTGQA_OK ? rc : launch(verify_select_kernel<DT>, dim3(num_seqs), dim3(64), 0, st, a);
 }
 
-// How a common-prefix call is cut into pieces; the same for its workspace and its launch.
-struct CommonPlan {
-    int p_row_waves, p_tiles, p_splits, p_keys, s_row_waves, s_shares;
-    int64_t rows, p_slots, p_units, s_workgroups;                // s_workgroups: own pieces at most
-    int64_t p_pieces(int num_kv_heads) const { return num_kv_heads * p_splits * p_slots; }
-    int64_t workgroups() const { return (p_units + 7) / 8 * 8 * p_tiles + s_workgroups; }
-    int64_t pieces(int num_kv_heads) const { return p_pieces(num_kv_heads) + s_workgroups * s_row_waves; }
-    size_t bytes(int num_kv_heads, int head_dim) const { return (size_t)pieces(num_kv_heads) * 32 * (head_dim * sizeof(float) + sizeof(float2)); }
-};
-
-// Row blocks of a workgroup for so many rows: 1, 2 or 4 of 32.
-int common_row_waves(int64_t rows) { return rows > 64 ? 4 : rows > 32 ? 2 : 1; }
-
-// false: sizes beyond the kernels' 32-bit counts
-bool plan_common(CommonPlan& c, int64_t num_tokens, int64_t num_seqs, int num_heads, int num_kv_heads, int64_t prefix_len, int64_t max_context_len,
-                 int64_t max_q_len)
-{
-    const int64_t group = num_heads / num_kv_heads, cus = num_cus();
-    c = CommonPlan{};
-    c.rows = num_tokens * group;
-    c.p_slots = (c.rows + 31) / 32;
-    c.p_row_waves = common_row_waves(c.rows);
-    c.p_tiles = 1, c.p_keys = 32;
-    if (c.rows >= (1ll << 31) - 64 || c.p_slots * num_kv_heads >= (1ll << 31)) return false;
-    // A workgroup of each kind to a CU: the prefix's is bound by its matrix and vector instructions, the own parts' by memory.
-    if (prefix_len > 0) {
-        c.p_tiles = (int)((c.p_slots + c.p_row_waves - 1) / c.p_row_waves);
-        // ranges: none shorter than two tiles of 32 for each key group of a workgroup
-        const int64_t step = 32 * (kCommonWaves / c.p_row_waves), units = (int64_t)num_kv_heads * c.p_tiles;
-        const int64_t n = std::max<int64_t>(std::min(cus / units, prefix_len / (2 * step)), 1);
-        const int64_t each = ((prefix_len + n - 1) / n + step - 1) / step * step;
-        c.p_keys = (int)each;
-        c.p_splits = (int)((prefix_len + each - 1) / each);
-        c.p_units = (int64_t)num_kv_heads * c.p_splits;
-    }
-    const int64_t behind = max_context_len - prefix_len, own_rows = std::min(max_q_len, num_tokens) * group;
-    c.s_row_waves = common_row_waves(own_rows);
-    if (behind > 0) {
-        const int64_t tile_rows = 32 * c.s_row_waves, step = 32 * (kCommonWaves / c.s_row_waves);
-        // row tiles: of all sequences at the bound, or of all tokens and one begun by each sequence
-        const int64_t tiles = std::min(num_seqs * ((own_rows + tile_rows - 1) / tile_rows), c.rows / tile_rows + num_seqs);
-        const int64_t each = (behind + step - 1) / step, steps = num_kv_heads * tiles * each;
-        if (each > (1 << 20) || steps >= (1ll << 30)) return false;
-        // (a piece of half of all CUs' share: with more pieces, and with fewer, 64 sequences behind 4 096 tokens, own parts of 127 - 1 023, take
-        // 37 - 38 us instead of 32, behind 32 768, 1 023 - 2 047, 110 - 125 instead of 110)
-        c.s_shares = (int)std::min<int64_t>(std::max<int64_t>(cus / 2, 1), steps);
-        // no more than the shares and one for each segment
-        c.s_workgroups = c.s_shares + num_kv_heads * (c.rows / tile_rows + num_seqs);
-    }
-    return c.workgroups() < (1ll << 31);
-}
-
 template <int DT, bool KV8, int D>
 int launch_common(const CommonParams& p, int workgroups, hipStream_t st)
 {
@@ -254,8 +203,8 @@ int common_impl(void* out, const void* q, const void* k_cache, const void* v_cac
         return OPTGQA_ERR_NULL;
     if (!aligned16(out) || !aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache)) return OPTGQA_ERR_UNSUPPORTED;
     CommonPlan c;
-    if (!plan_common(c, num_tokens, num_seqs, num_heads, num_kv_heads, prefix_len, max_context_len, cu_q_lens ? max_q_len : 1)) return OPTGQA_ERR_SHAPE;
-    if (!workspace || !aligned16(workspace) || workspace_bytes < c.bytes(num_kv_heads, head_dim)) return OPTGQA_ERR_WORKSPACE;
+    if (!plan_common(c, num_tokens, num_seqs, num_heads, num_kv_heads, prefix_len, max_context_len, cu_q_lens ? max_q_len : 1, num_cus())) return OPTGQA_ERR_SHAPE;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < c.bytes(head_dim)) return OPTGQA_ERR_WORKSPACE;
 
     CommonParams p;
     p.out = out;
@@ -450,15 +399,15 @@ int optgqa_verify_drafts(int64_t* tokens, int32_t* num_accepted, const void* tar
 size_t optgqa_common_prefix_workspace_bytes(int num_tokens, int num_seqs, int num_heads, int num_kv_heads, int head_dim,
                                             int block_size, int num_prefix_blocks, int max_context_len, int max_q_len)
 {
-    if (num_tokens <= 0 || num_seqs <= 0 || num_heads <= 0 || num_kv_heads <= 0 || num_heads % num_kv_heads || !head_dim_ok(head_dim) ||
+    if (num_tokens <= 0 || num_seqs <= 0 || num_heads <= 0 || num_heads > 65535 || num_kv_heads <= 0 || num_heads % num_kv_heads || !head_dim_ok(head_dim) ||
         !block_size_ok(block_size) || num_prefix_blocks < 0 || max_context_len < 0 || max_q_len <= 0)
         return 0;
     // (without prefix sums of new tokens a sequence has one, whatever the bound: the call needs the larger of the two)
     size_t bytes = 16;
     for (const int n : {max_q_len, 1}) {
         CommonPlan c;
-        if (!plan_common(c, num_tokens, num_seqs, num_heads, num_kv_heads, (int64_t)num_prefix_blocks * block_size, max_context_len, n)) return 0;
-        bytes = std::max(bytes, c.bytes(num_kv_heads, head_dim));
+        if (!plan_common(c, num_tokens, num_seqs, num_heads, num_kv_heads, (int64_t)num_prefix_blocks * block_size, max_context_len, n, num_cus())) return 0;
+        bytes = std::max(bytes, c.bytes(head_dim));
     }
     return bytes;
 }

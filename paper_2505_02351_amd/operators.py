@@ -186,7 +186,7 @@ def rotary_and_cache_fp8_heads(q_out: torch.Tensor, q: torch.Tensor, k: torch.Te
 
 def common_prefix_workspace_bytes(num_tokens: int, num_seqs: int, num_heads: int, num_kv_heads: int, head_dim: int, block_size: int,
                                   num_prefix_blocks: int, max_context_len: int, max_q_len: int = 1) -> int:
-    """optgqa_common_prefix_workspace_bytes."""
+    """optgqa_common_prefix_workspace_bytes: sized for the largest of each argument, a workspace serves every call."""
     return int(_pkg.load_library().optgqa_common_prefix_workspace_bytes(num_tokens, num_seqs, num_heads, num_kv_heads, head_dim, block_size,
                                                                         num_prefix_blocks, max_context_len, max_q_len))
 
