@@ -65,14 +65,15 @@ struct CommonParams {
     int num_tokens, num_seqs, num_heads, num_kv_heads, group, block_shift, max_blocks_per_seq;
     int prefix_len;             // keys
     int rows;                   // num_tokens * group: of a KV head
-    int p_row_waves, p_tiles, p_splits, p_keys, p_units, p_workgroups;      // tiles: workgroups' row tiles; units: KV head, range
+    int p_row_waves, p_tiles, p_splits, p_keys;                              // tiles: workgroups' row tiles; splits: ranges of p_keys keys
     int s_row_waves, s_shares;
     // pieces, 32 rows each: of the prefix [range][KV head][p_slots]; then s_row_waves for each own one
     int p_slots;
     int64_t s_first;
     float4* o;                  // per piece [D / 8][64]: what lane l of the wave holds, dims 8i + 4 (l / 32) .. + 3 of row l % 32
     float2* ml;                 // per piece [32]: m, l
-    FastDiv by_group, by_p_tiles, by_kv_heads, by_s_shares;
+    PrefixItems p_items;
+    FastDiv by_group, by_kv_heads, by_s_shares;
 };
 
 template <int D, bool KV8> constexpr int kCommonLds = [] {
@@ -605,15 +606,12 @@ __global__ __launch_bounds__(kCommonThreads, 2) void common_prefix_kernel(const 
 {
     const int lane = threadIdx.x & 63;
     CommonJob job;
-    job.prefix = (int)blockIdx.x < p.p_workgroups;
+    const int p_workgroups = p.p_items.workgroups();
+    job.prefix = (int)blockIdx.x < p_workgroups;
     const int row_waves = job.prefix ? p.p_row_waves : p.s_row_waves;
     if (job.prefix) {
-        // workgroups go to XCD (number % 8): the row tiles of one (KV head, range of keys), which read the same tiles, to one
-        const int x = blockIdx.x & 7, w = blockIdx.x >> 3, unit8 = p.by_p_tiles.div(w);
-        const int unit = unit8 * 8 + x, tile = w - unit8 * p.p_tiles;
-        if (unit >= p.p_units) return;
-        const int range = p.by_kv_heads.div(unit);
-        job.g = unit - range * p.num_kv_heads;
+        int range, tile;
+        if (!p.p_items.place(blockIdx.x, p.p_splits, p.p_tiles, job.g, range, tile)) return;
         job.table = p.prefix_table;
         job.kbeg = range * p.p_keys;
         job.kend = min(job.kbeg + p.p_keys, p.prefix_len);
@@ -622,7 +620,7 @@ __global__ __launch_bounds__(kCommonThreads, 2) void common_prefix_kernel(const 
         job.tok0 = job.pos0 = 0;
         job.slot = ((int64_t)range * p.num_kv_heads + job.g) * p.p_slots + tile * row_waves;
     } else {
-        const int me = blockIdx.x - p.p_workgroups;              // the piece
+        const int me = blockIdx.x - p_workgroups;              // the piece
         OwnParts parts(p, 0);
         const int share = own_share(p, parts);
         int all = 0, from = 0;

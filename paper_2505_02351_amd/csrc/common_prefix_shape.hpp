@@ -6,16 +6,41 @@
 
 #include <algorithm>
 
+#include "common.hpp"
+
 namespace optgqa {
 
-constexpr int kCommonThreads = 256, kCommonWaves = 4;
+constexpr int kCommonThreads = 256, kCommonWaves = 4, kCommonXcds = 8;
+
+// The prefix's part of a launch: an item for each (KV head, range of keys, row tile), by KV head, then range, then tile.  Workgroups go to
+// XCD (number % 8), which has an L2 of its own: each XCD takes an eighth of the items, one behind another, so that the tiles of a
+// range, which read the same keys, and the ranges of a KV head, which read the same queries, are together as far as
+// all XCDs have as much to do.
+struct PrefixItems {
+    int items, per_xcd;
+    FastDiv by_tiles, by_ranges;
+    __host__ void set(int kv_heads, int ranges, int tiles)
+    {
+        items = kv_heads * ranges * tiles, per_xcd = (items + kCommonXcds - 1) / kCommonXcds;
+        by_tiles.set((uint32_t)tiles), by_ranges.set((uint32_t)(ranges > 0 ? ranges : 1));
+    }
+    __host__ __device__ __forceinline__ int workgroups() const { return per_xcd * kCommonXcds; }
+    // of a workgroup below workgroups(); false: it has none
+    __host__ __device__ __forceinline__ bool place(int workgroup, int ranges, int tiles, int& g, int& range, int& tile) const
+    {
+        const int item = workgroup % kCommonXcds * per_xcd + workgroup / kCommonXcds, unit = by_tiles.div(item);
+        g = by_ranges.div(unit);
+        range = unit - g * ranges, tile = item - unit * tiles;
+        return item < items;
+    }
+};
 
 struct CommonPlan {
     int p_row_waves, p_tiles, p_splits, p_keys, s_row_waves, s_shares;
     int64_t rows, p_slots, p_units, s_workgroups;                // s_workgroups: own pieces at most
     int64_t held;                                                // pieces of 32 rows that the workspace has to hold
     int64_t p_pieces(int num_kv_heads) const { return num_kv_heads * p_splits * p_slots; }
-    int64_t workgroups() const { return (p_units + 7) / 8 * 8 * p_tiles + s_workgroups; }
+    int64_t workgroups() const { return (p_units * p_tiles + kCommonXcds - 1) / kCommonXcds * kCommonXcds + s_workgroups; }
     int64_t pieces(int num_kv_heads) const { return p_pieces(num_kv_heads) + s_workgroups * s_row_waves; }
     size_t bytes(int head_dim) const { return (size_t)held * 32 * (head_dim * sizeof(float) + 2 * sizeof(float)); }
 };

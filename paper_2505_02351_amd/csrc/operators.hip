@@ -239,8 +239,7 @@ int common_impl(void* out, const void* q, const void* k_cache, const void* v_cac
     p.p_tiles = c.p_tiles;
     p.p_splits = c.p_splits;
     p.p_keys = c.p_keys;
-    p.p_units = (int)c.p_units;
-    p.p_workgroups = (int)((c.p_units + 7) / 8 * 8 * c.p_tiles);
+    p.p_items.set(num_kv_heads, c.p_splits, c.p_tiles);
     p.s_row_waves = c.s_row_waves;
     p.s_shares = c.s_shares;
     p.p_slots = (int)c.p_slots;
@@ -249,7 +248,6 @@ int common_impl(void* out, const void* q, const void* k_cache, const void* v_cac
     p.o = static_cast<float4*>(workspace);
     p.ml = reinterpret_cast<float2*>(static_cast<unsigned char*>(workspace) + pieces * 32 * head_dim * sizeof(float));
     p.by_group.set((uint32_t)p.group);
-    p.by_p_tiles.set((uint32_t)c.p_tiles);
     p.by_kv_heads.set((uint32_t)num_kv_heads);
     p.by_s_shares.set((uint32_t)std::max(c.s_shares, 1));
     hipStream_t st = static_cast<hipStream_t>(stream);

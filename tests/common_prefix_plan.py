@@ -12,8 +12,8 @@ Plan = collections.namedtuple("Plan", "row_waves row_tiles ranges keys own_row_w
 def build(folder):
     """The rules as a shared library in `folder`."""
     out = str(folder / "libcommon_prefix.so")
-    subprocess.run([os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "llvm", "bin", "clang++"), "-std=c++17", "-O1", "-fPIC", "-shared", "-I" + CSRC,
-                    os.path.join(HERE, "host_hip", "common_prefix.cpp"), "-o", out], check=True)
+    subprocess.run([os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "llvm", "bin", "clang++"), "-std=c++17", "-O1", "-fPIC", "-shared", "-Wno-ignored-attributes",
+                    "-I" + os.path.join(HERE, "host_hip"), "-I" + CSRC, os.path.join(HERE, "host_hip", "common_prefix.cpp"), "-o", out], check=True)
     lib = ctypes.CDLL(out)
     lib.common_plan_of.argtypes = [ctypes.c_int64] * 2 + [ctypes.c_int] * 2 + [ctypes.c_int64] * 4 + [ctypes.c_void_p]
     return lib

@@ -13,3 +13,13 @@ extern "C" int common_plan_of(int64_t num_tokens, int64_t num_seqs, int num_head
     for (int i = 0; i < 8; ++i) out[i] = all[i];
     return 1;
 }
+
+// Where the prefix's workgroups of a launch find their work: out[3 n ..] = KV head, range, row tile, or -1.  The number of workgroups.
+extern "C" int common_prefix_places(int kv_heads, int ranges, int tiles, int32_t* out)
+{
+    PrefixItems items;
+    items.set(kv_heads, ranges, tiles);
+    for (int n = 0; out && n < items.workgroups(); ++n)
+        if (!items.place(n, ranges, tiles, out[3 * n], out[3 * n + 1], out[3 * n + 2])) out[3 * n] = out[3 * n + 1] = out[3 * n + 2] = -1;
+    return items.workgroups();
+}
