@@ -147,10 +147,17 @@ int rotary_and_cache_impl(void* q_out, const void* q, const void* k, const void*
     return rotary_impl(c, scales ? RotaryTo::kCacheE4M3 : RotaryTo::kCache, static_cast<hipStream_t>(stream));
 }
 
+// Whether calls on this stream are recorded for a graph (the null stream never is).
+bool is_captured(hipStream_t st)
+{
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    return st && hipStreamIsCapturing(st, &status) == hipSuccess && status == hipStreamCaptureStatusActive;
+}
+
 template <int DT>
 int launch_verify(const VerifyParams& a, int num_seqs, hipStream_t st)
 {
-    if (a.chunks <= kVerifyOneChunks)
+    if (a.chunks <= kVerifyOneChunks && !(a.chunks > kVerifyOneQuick && num_seqs < kVerifyOneSeqs && is_captured(st)))
         return launch(verify_one_kernel<DT>, dim3(num_seqs), dim3(64 * kVerifyOneWaves), 0, st, a);
     constexpr int kWaves = kVerifyThreads / 64;
     const int rc = launch(verify_sums_kernel<DT>, dim3(num_seqs, (a.chunks + kWaves - 1) / kWaves), dim3(kVerifyThreads), 0, st, a);

@@ -8,7 +8,7 @@
 // Bound by memory: one row of p and one of q per sequence, everything else is a few scattered entries.  Rows are long
 // (10^4 to 10^5 entries) and sequences few, so a row is cut into chunks of 1 024 entries, a wave each, with all its loads in
 // flight at once; they leave their sums.  In a second launch a wave for each sequence looks up the chunk that the draw falls in and reads
-// that one again; rows of up to 32 chunks have both in one.  What is left is latency: three dependent round trips to memory to judge the drafts, one for the row, then two in the second
+// that one again; rows of up to 32 chunks mostly have both in one.  What is left is latency: three dependent round trips to memory to judge the drafts, one for the row, then two in the second
 // launch.
 // Measured: 64 sequences of 128 255 entries, fp32: 17.5 us (kernels 13.2, 5.0 TB/s, and 4.5); one of 32 000: 8.7, the call.
 #pragma once
@@ -240,11 +240,17 @@ __global__ __launch_bounds__(64) void verify_select_kernel(const VerifyParams a)
     select_token<DT>(a, b, a.cu[b], a.verdicts[b], a.sums + (int64_t)b * a.chunks);
 }
 
-// Both in one launch, for rows of up to two chunks to each of a workgroup's sixteen waves.  Us a call, and of GPU time, two launches against
-// one, fp32: one sequence of 4 096 entries 10.7 -> 8.5 and 6.6 -> 5.4, of 32 000 10.6 -> 8.7 and 7.2 -> 8.7 (the second chunk's loads wait
-// for the first's; more of them under way in straight code: 9.0, that code has to be fetched), 64 of 16 000 10.6 -> 8.4 and 8.5 -> 7.8, 256
-// of 32 000 17.5 -> 14.3 and 17.7 -> 14.4.
-constexpr int kVerifyOneWaves = 16, kVerifyOneChunks = 2 * kVerifyOneWaves;
+// Both in one launch, for rows of up to two chunks to each of a workgroup's sixteen waves; the same bits.  A call on a stream is bound by its
+// launches, and one is always the faster (one sequence of 4 096 entries, fp32: 9.4 us against 12.2, of 32 000 9.4 / 12.2, 64 of 16 000 9.5 / 12.2,
+// 256 of 32 000 14.6 / 17.7).  In a graph only the GPU's time counts, and there a workgroup has one CU for a sequence's chunks where two
+// launches have one for every four.  Us in a replayed graph, one launch against two, fp32:
+//     sequences   16 chunks    20           22           24           28           32
+//       1         6.3 / 6.7   6.8 / 6.8    7.1 / 6.8    7.1 / 6.7    7.8 / 6.8    8.3 / 6.7
+//      32                     7.2 / 7.5    7.6 / 7.5    7.5 / 7.4    8.1 / 7.6    8.9 / 7.5
+//      64         7.7 / 8.3   7.6 / 8.3    8.3 / 8.8    8.5 / 8.8    9.1 / 9.3   10.1 / 9.6
+//     128                     9.0 / 10.8   9.3 / 11.0   9.4 / 11.1   9.9 / 11.9  10.9 / 12.4
+// so a captured call has two where chunks are more than 20 and sequences fewer than 64.
+constexpr int kVerifyOneWaves = 16, kVerifyOneChunks = 2 * kVerifyOneWaves, kVerifyOneQuick = 20, kVerifyOneSeqs = 64;
 template <int DT>
 __global__ __launch_bounds__(64 * kVerifyOneWaves) void verify_one_kernel(const VerifyParams a)
 {
