@@ -590,7 +590,8 @@ int optgqa_rotary_frequencies_host(double *freqs_host, float *magnitude_host, in
  *   prefix_table    [num_prefix_blocks] int32, full blocks; num_prefix_blocks may be 0
  *   cu_q_lens       [num_seqs + 1] int32 prefix sums, or NULL: one new token each (num_tokens == num_seqs)
  *   max_context_len, max_q_len   upper bounds on the context lengths (prefix included) and the n_b; they size the launch
- *                   (OPTGQA_ERR_SHAPE beyond 2^30 tokens, 2^25 behind the prefix)
+ *                   (OPTGQA_ERR_SHAPE beyond 2^30 tokens, 2^25 behind the prefix; also where num_tokens * num_heads reaches
+ *                   some 2^29, or num_seqs * num_kv_heads 2^24)
  *   workspace       optgqa_common_prefix_workspace_bytes(...) bytes, 16-byte aligned (OPTGQA_ERR_WORKSPACE without it).  The size
  *                   grows with every one of num_tokens, num_seqs, num_prefix_blocks, max_context_len and max_q_len: a
  *                   workspace for the largest of each serves every call
@@ -649,7 +650,7 @@ int optgqa_paged_attention_common_fp8_heads(void *out, const void *q, const void
  * tokens[b] = kept drafts, the drawn token, then -1; num_accepted[b] = the number of kept drafts.  Rows need not sum to 1.
  *
  *   tokens          [num_seqs][max_drafts + 1] int64
- *   num_accepted    [num_seqs] int32
+ *   num_accepted    [num_seqs] int32 (num_seqs: fewer than 2^22)
  *   target_probs    [cu_draft_lens[num_seqs] + num_seqs][vocab_size] of dtype (OPTGQA_F32 too), rows target_stride
  *                   (>= vocab_size) elements apart; draft_probs likewise, one row per draft
  *   draft_tokens    int64, accept_uniforms fp32 in [0, 1): one per draft (NULL: there are none)

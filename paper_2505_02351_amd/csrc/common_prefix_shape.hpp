@@ -11,6 +11,7 @@
 namespace optgqa {
 
 constexpr int kCommonThreads = 256, kCommonWaves = 4, kCommonXcds = 8;
+constexpr int64_t kCommonMostWorkgroups = 0xffffffffLL / kCommonThreads;         // a dimension of a launch has fewer than 2^32 threads
 
 // The prefix's part of a launch: an item for each (KV head, range of keys, row tile), by KV head, then range, then tile.  Workgroups go to
 // XCD (number % 8), which has an L2 of its own: each XCD takes an eighth of the items, one behind another, so that the tiles of a
@@ -71,7 +72,7 @@ inline int64_t common_held(int64_t rows, int64_t num_seqs, int64_t own_rows, int
     return prefix + own;
 }
 
-// false: sizes beyond the kernels' 32-bit counts
+// false: sizes beyond the kernels' 32-bit counts or a launch's workgroups
 inline bool plan_common(CommonPlan& c, int64_t num_tokens, int64_t num_seqs, int num_heads, int num_kv_heads, int64_t prefix_len, int64_t max_context_len,
                         int64_t max_q_len, int64_t cus)
 {
@@ -81,7 +82,7 @@ inline bool plan_common(CommonPlan& c, int64_t num_tokens, int64_t num_seqs, int
     c.p_slots = (c.rows + 31) / 32;
     c.p_row_waves = common_row_waves(c.rows);
     c.p_tiles = 1, c.p_keys = 32;
-    if (c.rows >= (1ll << 31) - 64 || c.p_slots * num_kv_heads >= (1ll << 31)) return false;
+    if (c.rows >= (1ll << 31) - 64 || c.p_slots * num_kv_heads > kCommonMostWorkgroups) return false;        // (the join's)
     // A workgroup of each kind to a CU: the prefix's is bound by its matrix and vector instructions, the own parts' by memory.
     if (prefix_len > 0) {
         c.p_tiles = (int)((c.p_slots + c.p_row_waves - 1) / c.p_row_waves);
@@ -107,7 +108,7 @@ inline bool plan_common(CommonPlan& c, int64_t num_tokens, int64_t num_seqs, int
         // no more than the shares and one for each segment
         c.s_workgroups = c.s_shares + num_kv_heads * (c.rows / tile_rows + num_seqs);
     }
-    if (c.workgroups() >= (1ll << 31)) return false;
+    if (c.workgroups() > kCommonMostWorkgroups) return false;
     c.held = common_held(c.rows, num_seqs, own_rows, num_kv_heads, prefix_len, max_context_len, cus);
     return true;
 }

@@ -16,6 +16,9 @@ inline bool head_dim_ok(int d) { return d == 64 || d == 128; }
 inline bool block_size_ok(int bs) { return bs == 16 || bs == 32 || bs == 64; }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// Workgroups of so many threads that one dimension of a launch may have: fewer than 2^32 threads.
+constexpr int64_t most_workgroups(int threads) { return 0xffffffffLL / threads; }
+
 // Launch through the call that reports THIS launch's own status (hipLaunchKernel): an error
 // some earlier work of the caller left behind in the runtime's "last error" slot is neither
 // reported as ours nor cleared.
@@ -23,6 +26,8 @@ template <typename... KArgs, typename... Args>
 int launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t lds_bytes, hipStream_t st, Args&&... args)
 {
     static_assert(sizeof...(KArgs) == sizeof...(Args), "argument count does not match the kernel");
+    // (the runtime takes a dimension of 2^32 threads and more without a word, and runs what is left of it modulo 2^32)
+    if ((uint64_t)grid.x * block.x >> 32 || (uint64_t)grid.y * block.y >> 32 || (uint64_t)grid.z * block.z >> 32) return OPTGQA_ERR_LAUNCH;
     std::tuple<std::decay_t<KArgs>...> vals(std::forward<Args>(args)...);
     void* ptrs[sizeof...(KArgs)];
     std::apply([&](auto&... v) { int i = 0; ((ptrs[i++] = static_cast<void*>(&v)), ...); }, vals);

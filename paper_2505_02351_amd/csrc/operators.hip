@@ -82,15 +82,8 @@ int rotary_impl(const RotaryCall& c, RotaryTo to, hipStream_t st)
                       (c.q_stride | c.q_out_stride | c.k_stride | c.k_out_stride | c.v_stride) % 8 == 0;
 
     RotaryParams p;
-    p.q = c.q;
-    p.q_out = c.q_out;
-    p.k = c.k;
-    p.k_out = c.k_out;
-    p.v = c.v;
     p.k_cache = c.k_cache;
     p.v_cache = c.v_cache;
-    p.slots = c.slots;
-    p.positions = c.positions;
     p.freqs = c.freqs;
     p.q_stride = c.q_stride;
     p.q_out_stride = c.q_out_stride;
@@ -109,7 +102,6 @@ int rotary_impl(const RotaryCall& c, RotaryTo to, hipStream_t st)
             p.v_inv_scale = 1.0f / c.scales->v;
         }
     }
-    p.num_tokens = c.num_tokens;
     p.q_heads = c.num_heads;
     p.kv_heads = c.num_kv_heads;
     p.heads = c.num_heads + c.num_kv_heads * (store ? 2 : 1);
@@ -130,11 +122,26 @@ int rotary_impl(const RotaryCall& c, RotaryTo to, hipStream_t st)
     }
     p.by_heads_per_wg.set((uint32_t)p.heads_per_wg);
     p.by_pairs.set((uint32_t)p.pairs);
-    const dim3 grid((unsigned)(((int64_t)c.num_tokens + p.tokens_per_wg - 1) / p.tokens_per_wg),
-                    (unsigned)((p.heads + p.heads_per_wg - 1) / p.heads_per_wg));
-    if (to == RotaryTo::kRows) return launch_rotary<RotaryTo::kRows>(p, c.dtype, c.interleaved != 0, wide, grid, st);
-    if (to == RotaryTo::kCache) return launch_rotary<RotaryTo::kCache>(p, c.dtype, c.interleaved != 0, wide, grid, st);
-    return launch_rotary<RotaryTo::kCacheE4M3>(p, c.dtype, c.interleaved != 0, wide, grid, st);
+    // slices of tokens, one but for 2^24 and more
+    const int64_t most = most_workgroups(kRotaryThreads) * p.tokens_per_wg;
+    auto from = [](auto* at, int64_t bytes) { return at ? reinterpret_cast<decltype(at)>(reinterpret_cast<uintptr_t>(at) + bytes) : at; };
+    for (int64_t first = 0; first < c.num_tokens; first += most) {
+        p.q = from(c.q, first * c.q_stride * 2);
+        p.q_out = from(c.q_out, first * c.q_out_stride * 2);
+        p.k = from(c.k, first * c.k_stride * 2);
+        p.k_out = from(c.k_out, first * c.k_out_stride * 2);
+        p.v = from(c.v, first * c.v_stride * 2);
+        p.slots = c.slots ? c.slots + first : nullptr;
+        p.positions = c.positions + first;
+        p.num_tokens = (int)std::min(c.num_tokens - first, most);
+        const dim3 grid((unsigned)(((int64_t)p.num_tokens + p.tokens_per_wg - 1) / p.tokens_per_wg),
+                        (unsigned)((p.heads + p.heads_per_wg - 1) / p.heads_per_wg));
+        const int rc = to == RotaryTo::kRows    ? launch_rotary<RotaryTo::kRows>(p, c.dtype, c.interleaved != 0, wide, grid, st)
+                       : to == RotaryTo::kCache ? launch_rotary<RotaryTo::kCache>(p, c.dtype, c.interleaved != 0, wide, grid, st)
+                                                : launch_rotary<RotaryTo::kCacheE4M3>(p, c.dtype, c.interleaved != 0, wide, grid, st);
+        if (rc != OPTGQA_OK) return rc;
+    }
+    return OPTGQA_OK;
 }
 
 int rotary_and_cache_impl(void* q_out, const void* q, const void* k, const void* v, void* k_cache, void* v_cache,
@@ -369,7 +376,7 @@ int optgqa_verify_drafts(int64_t* tokens, int32_t* num_accepted, const void* tar
         return OPTGQA_ERR_SHAPE;
     if (!dtype_ok(dtype) && dtype != OPTGQA_F32) return OPTGQA_ERR_UNSUPPORTED;
     const int chunks = (int)(((int64_t)vocab_size + kVerifyChunk - 1) / kVerifyChunk);
-    if (chunks > 4 * 65535) return OPTGQA_ERR_SHAPE;             // (2^28 entries)
+    if (chunks > 4 * 65535 || num_seqs > most_workgroups(64 * kVerifyOneWaves)) return OPTGQA_ERR_SHAPE;     // (2^28 entries, 2^22 sequences)
     if (num_seqs == 0) return OPTGQA_OK;
     if (!tokens || !num_accepted || !target_probs || !cu_draft_lens || !sample_uniforms)
         return OPTGQA_ERR_NULL;
