@@ -193,15 +193,14 @@ def _workspace(ws: Optional[torch.Tensor], ref: torch.Tensor) -> int:
     return ws.numel() * ws.element_size()
 
 
-def _typed(ref: torch.Tensor, *, same=(), u8=(), i32=(), i64=(), f32=(), f64=()) -> None:
+def _typed(ref: torch.Tensor, *, same=(), u8=(), i32=(), i64=(), f32=()) -> None:
     """Refuse, before any pointer is taken, what the C ABI cannot check: the library reads raw
     device pointers, so a tensor of another element type or on another device would be misread
     (block ids and slots out of range make the kernels write out of bounds).  ``ref`` (q, or k for
     the cache writes) fixes the 2-byte type and the device; each group is a list of (name, tensor
     or None).  Element types first (TypeError), then devices (ValueError)."""
     _dtype_code(ref)
-    groups = ((same, ref.dtype), (u8, torch.uint8), (i32, torch.int32), (i64, torch.int64), (f32, torch.float32),
-              (f64, torch.float64))
+    groups = ((same, ref.dtype), (u8, torch.uint8), (i32, torch.int32), (i64, torch.int64), (f32, torch.float32))
     for group, want in groups:
         for name, t in group:
             if t is None:
