@@ -378,8 +378,11 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
         if (__builtin_amdgcn_ballot_w64(first || mx > CommonSoftmax<DT>::kThreshold) != 0) {
             mx = fmaxf(mx, __shfl_xor(mx, 32));                  // the row's keys live in 2 lanes (h2)
             const bool sees = mx > -INFINITY;
+            float to = mx + CommonSoftmax<DT>::kHeadroom;
+            // (beyond 2^27 this rounds by more than there is room for above the threshold)
+            if (CommonSoftmax<DT>::kHeadroom < 0.f && mx - to > CommonSoftmax<DT>::kThreshold) to = mx;
             // (0 for a row that did not ask: no row's bits depend on what its neighbours hold)
-            const float delta = (first ? sees : mx > CommonSoftmax<DT>::kThreshold) ? mx + CommonSoftmax<DT>::kHeadroom : 0.f;
+            const float delta = (first ? sees : mx > CommonSoftmax<DT>::kThreshold) ? to : 0.f;
             const float alpha = first ? 1.f : fast_exp2(-delta);
             started = started || sees;
             m_ref += delta;
