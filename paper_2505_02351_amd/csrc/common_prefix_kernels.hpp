@@ -323,7 +323,6 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
     for (int m = 0; m < kQ; ++m) qb[m] = make_uint4(qb[m].x & keep_q, qb[m].y & keep_q, qb[m].z & keep_q, qb[m].w & keep_q);
     const float scale2 = KV8 && p.k_scales ? p.scale2 * p.k_scales[job.g] : p.scale2;
     const float slope2 = row_ok ? slope * kLog2e : 0.f;
-    const float posf = (float)pos;
     f32x16 key_bias;                                             // slope * (key's offset in its tile) / score scale: the scores start from it
     {
         const float per_key = slope2 / scale2;
@@ -364,7 +363,7 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
     // key0: the tile's first key
     auto softmax = [&](int key0, f32x16 st, auto masked) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(masked)::value;
-        const float b0 = fmaf(slope2, (float)(key0 + 4 * h2) - posf, -m_ref);
+        const float b0 = fmaf(slope2, (float)(key0 + 4 * h2 - pos), -m_ref);         // (whole numbers' difference: exact near the row, however far)
         float x[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
