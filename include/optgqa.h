@@ -582,7 +582,8 @@ int optgqa_rotary_frequencies_host(double *freqs_host, float *magnitude_host, in
  * already cached, at positions context_lens[b] - n_b .. context_lens[b] - 1; each sees the keys up to its own position:
  *     s_j = scale * <q, K_g[j]> + alibi_slopes[h] * (j - pos), j = 0 .. pos;   out = sum_j softmax(s)_j V_g[j]
  * - what optgqa_paged_attention (n_b = 1) and optgqa_paged_prefill give on full tables, to rounding - for decode steps, for
- * drafted tokens that are verified together (n_b = drafts + 1), and for chunks.  The prefix's keys are read once for 128 rows
+ * drafted tokens that are verified together (n_b = drafts + 1), and for short chunks (of some 30 000 and more token-head
+ * rows, num_tokens * num_heads, optgqa_paged_prefill on full tables is the faster).  The prefix's keys are read once for 128 rows
  * (new tokens x heads of a group) of any sequences, as matrix products.  A context may be shorter than the prefix;
  * a row that sees no key (a negative position, or a token behind cu_q_lens[num_seqs]) is +0.
  *

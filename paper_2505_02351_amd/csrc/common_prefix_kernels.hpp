@@ -16,12 +16,13 @@
 // tiles of 32 keys in LDS; the KS groups take tiles in turn, and their results are joined through LDS.  With many rows 4 x 1 reads
 // each tile once for 128 rows, with few (a sequence's own part: the heads of a group, times its new tokens) 1 x 4 lets each wave
 // stream tiles of its own.  Scores, softmax and output as in prefill_kernels.hpp: both contractions transposed on
-// v_mfma_f32_32x32x16, sums and output in fp32, weights rounded to fp16 once or split into two bf16.
+// v_mfma_f32_32x32x16, sums and output in fp32, weights rounded to fp16 once (CommonSoftmax) or split into two bf16.
 //
-// Own parts are bound by memory, the prefix by its matrix instructions, their LDS reads (half of a CU's cycles) and the softmax between them,
-// short launches by their chains of loads.  Measured (both launches, inputs in turn): 64 sequences, 32 / 8 heads of 128, bf16, behind 32 768 tokens, 1 023 - 2 047
-// own: 108 us, 5.0 TB/s; 32 / 4 heads behind 4 096, 127 - 1 023 own, slopes: 30.4; 16 of 2 - 9 drafts, 64 / 8 heads, fp16, behind 8 192: 44.6 us,
-// 480 TFLOP/s; 32 behind 8 192, E4M3 caches: 27.7.
+// Own parts are bound by memory, the prefix by its matrix instructions, their LDS reads and the softmax between them, which one wave to a SIMD does
+// one after another, short launches by their chains of loads.  Measured (both launches, inputs in turn): 64 sequences, 32 / 8 heads of 128, bf16, behind
+// 32 768 tokens, 1 023 - 2 047 own: 108 - 110 us, 5.0 TB/s; 32 / 4 heads behind 4 096, 127 - 1 023 own, slopes: 30 - 31; 16 of 2 - 9 drafts, 64 / 8 heads,
+// fp16, behind 8 192: 44.6 us, 480 TFLOP/s; 32 behind 8 192, E4M3 caches: 27.6 - 28.1.
+// (head_dim 128 with bf16 takes all 256 registers that two workgroups to a CU leave a wave, and one more, which lies in scratch.)
 #pragma once
 #include <type_traits>
 
@@ -165,7 +166,8 @@ __device__ __forceinline__ int own_share(const CommonParams& p, const OwnParts& 
 // maximum).  bf16: as everywhere.  fp16 weights are rounded once, and a range may be a whole long prefix whose many small
 // weights add up beside one large one: the reference lies below the maximum, so that weights down to 24 binary orders under the largest are
 // normal numbers and those down to 35 are there (2 above it, as in the prefill kernel: 12 and 23; 32 767 keys 21.25 orders under one
-// key came to 1.54e-2 in place of 1.30e-2).  The room up to 2^15 is what keeps rescales few: maxima that grow by less than 5 orders need none.
+// key came to 1.54e-2 in place of 1.30e-2).  The room up to 2^15 is what keeps rescales few: maxima that grow by less than 5 orders need none.  (16 of
+// 2 - 9 drafts, 64 / 8 heads, behind 8 192: scores of variance 1 44.3 -> 44.5 us, 16 45 -> 53, 100 53 -> 55; a threshold of 2^15.9 53, a reference 8 below 52.)
 template <int DT> struct CommonSoftmax { static constexpr float kThreshold = PfSoftmax<DT>::kThreshold, kHeadroom = PfSoftmax<DT>::kHeadroom; };
 template <> struct CommonSoftmax<kF16> { static constexpr float kThreshold = 15.f, kHeadroom = -10.f; };
 

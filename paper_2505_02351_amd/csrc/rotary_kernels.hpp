@@ -13,7 +13,7 @@
 // then take (token, head, piece) items.  A piece is 8 pairs - two 16-byte loads and stores - or, past those, 16 dims
 // that pass through; where rows do not lie on 16 bytes or rotary_dim is no multiple of 16, one pair.  (Measured, inputs in
 // turn: 20 480 tokens, 32 / 8 heads of 128, bf16: 76 us, 5.5 TB/s, a large copy reaches 5.1; 4 099 tokens, 40 / 8 heads, the gradient of
-// 64 interleaved dims, fp16: 21.6 us; 2 943 tokens into E4M3 caches 13.5 us; one token 2.3 us.  Non-temporal loads: 72, 22 and 17 us, and
+// 64 interleaved dims, fp16: 21.6 us; 2 943 tokens into E4M3 caches 13.5 us; one token 1.9 us.  Non-temporal loads: 72, 22 and 17 us, and
 // the rows of a step are what the projection before has just written, so they are not taken.)
 #pragma once
 #include "common.hpp"

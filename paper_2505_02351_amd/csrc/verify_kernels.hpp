@@ -10,7 +10,7 @@
 // flight at once; they leave their sums.  In a second launch a wave for each sequence looks up the chunk that the draw falls in and reads
 // that one again; rows of up to 32 chunks mostly have both in one.  What is left is latency: three dependent round trips to memory to judge the drafts, one for the row, then two in the second
 // launch.
-// Measured: 64 sequences of 128 255 entries, fp32: 17.5 us (kernels 13.2, 5.0 TB/s, and 4.5); one of 32 000: 8.7, the call.
+// Measured: 64 sequences of 128 255 entries, fp32: 17.6 us (kernels 13.5, 4.9 TB/s, and 4.3), bf16 17.3, certain drafts 14.1; one of 32 000: 8.6, the call.
 #pragma once
 #include "common.hpp"
 
