@@ -21,7 +21,7 @@
 // Own parts are bound by memory, the prefix by its matrix instructions, their LDS reads and the softmax between them, which one wave to a SIMD does
 // one after another, short launches by their chains of loads.  Measured (both launches, inputs in turn): 64 sequences, 32 / 8 heads of 128, bf16, behind
 // 32 768 tokens, 1 023 - 2 047 own: 108 - 110 us, 5.0 TB/s; 32 / 4 heads behind 4 096, 127 - 1 023 own, slopes: 30 - 31; 16 of 2 - 9 drafts, 64 / 8 heads,
-// fp16, behind 8 192: 44.6 us, 480 TFLOP/s; 32 behind 8 192, E4M3 caches: 27.6 - 28.1.
+// fp16, behind 8 192: 44.6 us, 480 TFLOP/s; 32 behind 8 192, E4M3 caches: 27.6 - 28.3.
 // (head_dim 128 with bf16 takes all 256 registers that two workgroups to a CU leave a wave, and one more, which lies in scratch.)
 #pragma once
 #include <type_traits>
