@@ -668,6 +668,83 @@ int optgqa_verify_drafts(int64_t *tokens, int32_t *num_accepted, const void *tar
                          size_t workspace_bytes, int dtype, void *stream);
 
 /*
+ * Pages of the caches.  A pool of num_blocks blocks is described by block tables [num_seqs][max_blocks_per_seq], context lengths
+ * [num_seqs] (the first ceil(length / block_size) entries of a row are in use, the others are neither read nor written) and
+ * reference counts [num_blocks]: how many entries in use hold a block; 0: it is free.  Everything that holds blocks of a
+ * pool has a row in the tables (a common prefix too).  An empty pool is all zeros.  The calls below keep the three in
+ * step on the device, so that nothing is waited for on the host and they can be captured into graphs; what moves in the caches they
+ * say as pairs of blocks (from, to), for optgqa_copy_blocks.  Results depend on the inputs alone.  Lengths below 0
+ * count as 0, above a row's room as that; entries that name no block of the pool are passed over.
+ *
+ * optgqa_resize_sequences: every sequence gets the length new_lens[b] (0: it ends).  First, blocks behind the new lengths are given
+ * back.  Then the growing sequences, in order, take blocks: for a last block that is not full and that others hold too, a new one
+ * in its place, with a pair (copy on write; if all who hold a block are about to write it, the last of them keeps it), and
+ * blocks for the new length.  The lowest free blocks are taken first.  Where not as many are free as are wanted, no
+ * sequence grows, and shorter ones are cut all the same.
+ *   slot_mapping    [num_slots] int64 or NULL: where the new tokens go, token i of sequence b (position old length + i) at
+ *                   slot_mapping[cu_new_lens[b] + i]; -1 for those of a sequence's cu_new_lens[b + 1] - cu_new_lens[b] that it
+ *                   did not grow by (the cache stores pass over such slots).  Slots from cu_new_lens[num_seqs] on are left
+ *   cu_new_lens     [num_seqs + 1] int32 prefix sums (NULL where slot_mapping is)
+ *   copies          [num_seqs][2] int32: the pairs, in order of their sequences.  They have to be copied before the new tokens are stored
+ *   counts          [2] int32: the number of pairs; blocks that were lacking (0: all sequences have their lengths)
+ *   max_change      an upper bound on |new length - old length|; it sizes the launch (a change beyond it is made all the same)
+ *   workspace       optgqa_resize_workspace_bytes(...) bytes, 16-byte aligned (OPTGQA_ERR_WORKSPACE without it)
+ *
+ * optgqa_fork_sequences: row i of tables_out [num_out][max_blocks_per_seq] and lens_out becomes row parents[i] of the old table, all of them
+ * at once; a parent outside 0 .. num_seqs - 1: an empty row.  Blocks are shared; a sequence that is nobody's parent is
+ * freed.  (Beams: parents as the search chose them.  Parallel samples: one parent several times.)  The new tables and lengths take
+ * the old ones' place and must not overlap them (OPTGQA_ERR_SHAPE).
+ *
+ * optgqa_compact_blocks: of U blocks in use the i-th highest goes to the i-th lowest free one, as long as that is below U, at
+ * most max_copies of them; tables and reference counts follow.  With max_copies >= num_blocks / 2 the blocks in use are
+ * 0 .. U - 1 afterwards; fewer: the highest blocks are freed first, and the next call goes on.
+ *   copies          [max_copies][2] int32;   counts [2] int32: the number of pairs, U
+ *   workspace       optgqa_compact_workspace_bytes(num_blocks) bytes, 16-byte aligned
+ *
+ * optgqa_copy_blocks: for the first *num_copies (at most max_copies) pairs (from, to) block `to` of every cache becomes a copy of block
+ * `from`.  No block may be written by one pair and read or written by another (the calls above make no such pairs).
+ *   caches          [num_caches] device pointers, in device memory: K and V caches of all layers, each num_blocks blocks of
+ *                   block_bytes (a multiple of 16), 16-byte aligned
+ *   num_copies      device, e.g. counts of the calls above
+ *
+ * optgqa_keep_tokens: of the tokens behind position start_lens[b] - a tree of drafts, optgqa_paged_attention_tree - those on the accepted
+ * branch come to the front: in all caches the row at start_lens[b] + paths[b][i] goes to start_lens[b] + i, for i <
+ * path_lens[b].  paths[b] ascends strictly.  Other rows keep their bits (cut the sequence to start_lens[b] + path_lens[b] afterwards).
+ *   paths           [num_seqs][max_path] int32;   num_seqs at most 65 535
+ *   element_bytes   2, or 1 for 8-bit caches
+ */
+size_t optgqa_resize_workspace_bytes(int num_seqs, int max_blocks_per_seq, int num_blocks);
+
+int optgqa_resize_sequences(int32_t *block_tables, int32_t *context_lens, int32_t *ref_counts,
+                            const int32_t *new_lens, int64_t *slot_mapping,
+                            const int32_t *cu_new_lens, int32_t *copies, int32_t *counts,
+                            int num_seqs, int max_blocks_per_seq, int num_blocks, int block_size,
+                            int num_slots, int max_change, void *workspace, size_t workspace_bytes,
+                            void *stream);
+
+int optgqa_fork_sequences(int32_t *tables_out, int32_t *lens_out, const int32_t *block_tables,
+                          const int32_t *context_lens, int32_t *ref_counts, const int32_t *parents,
+                          int num_out, int num_seqs, int max_blocks_per_seq, int num_blocks,
+                          int block_size, void *stream);
+
+size_t optgqa_compact_workspace_bytes(int num_blocks);
+
+int optgqa_compact_blocks(int32_t *block_tables, const int32_t *context_lens, int32_t *ref_counts,
+                          int32_t *copies, int32_t *counts, int num_seqs, int max_blocks_per_seq,
+                          int num_blocks, int block_size, int max_copies, void *workspace,
+                          size_t workspace_bytes, void *stream);
+
+int optgqa_copy_blocks(void *const *caches, int num_caches, const int32_t *copies,
+                       const int32_t *num_copies, int max_copies, int num_blocks,
+                       size_t block_bytes, void *stream);
+
+int optgqa_keep_tokens(void *const *caches, int num_caches, const int32_t *block_tables,
+                       const int32_t *start_lens, const int32_t *paths, const int32_t *path_lens,
+                       int num_seqs, int max_path, int max_blocks_per_seq, int num_blocks,
+                       int num_kv_heads, int head_dim, int block_size, int element_bytes,
+                       void *stream);
+
+/*
  * Diagnostic: un-page the cache (Section III-A: pages are only a re-arrangement of the
  * sequence).  k_out / v_out are [num_seqs][max_context_len][num_kv_heads][head_dim]; token j of
  * sequence b is copied bit for bit for j < context_lens[b]; other rows are left untouched.

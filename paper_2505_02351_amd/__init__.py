@@ -124,6 +124,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.optgqa_validate_tables_host.restype = i32
     lib.optgqa_validate_tables_host.argtypes = [vp, vp, i32, i32, i32, i32]
     operators.declare(lib)
+    pages.declare(lib)
     _lib = lib
     return lib
 
@@ -816,9 +817,12 @@ def validate_tables_host(block_tables, context_lens, block_size: int, num_blocks
                                                int(bt.shape[1]), int(block_size), int(num_blocks)))
 
 
-from . import operators  # noqa: E402  (uses the helpers above)
+from . import operators, pages  # noqa: E402  (they use the helpers above)
 from .operators import (  # noqa: E402, F401
     ROTARY_BASE, ROTARY_LINEAR, ROTARY_PLAIN, ROTARY_WAVELENGTH, ROTARY_YARN, common_prefix_workspace_bytes, paged_attention_common,
     paged_attention_common_fp8, paged_attention_common_fp8_heads, rotary_and_cache, rotary_and_cache_fp8, rotary_and_cache_fp8_heads,
     rotary_embedding, rotary_frequencies, verify_drafts, verify_drafts_workspace_bytes,
+)
+from .pages import (  # noqa: E402, F401
+    CacheSet, compact_blocks, compact_workspace_bytes, copy_blocks, fork_sequences, keep_tokens, resize_sequences, resize_workspace_bytes,
 )

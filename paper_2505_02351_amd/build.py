@@ -15,7 +15,7 @@ import sys
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "liboptgqa.hip")          # all of it in one file
-PARTS = ("optgqa.hip", "operators.hip")                   # what SRC includes, compiled side by side
+PARTS = ("optgqa.hip", "operators.hip", "pages.hip")      # what SRC includes, compiled side by side
 LIB = os.path.join(PKG, "liboptgqa.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 
