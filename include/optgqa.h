@@ -637,6 +637,69 @@ int optgqa_paged_attention_common_fp8_heads(void *out, const void *q, const void
                                             workspace_bytes, int dtype, void *stream);
 
 /*
+ * Attention of trees of new tokens: optgqa_paged_attention_common, where a new token does not see all new tokens before it but those
+ * that its mask says - the ancestors in a tree of drafts, or any others.  Sequence b's n_b new tokens lie at the positions base ..
+ * context_lens[b] - 1 of its cache, base = context_lens[b] - n_b, in the order of q.  Token i of them sees all keys below base, and
+ * the key at base + c where bit c of its mask is set (itself too only then); keys that it sees at j < base are j - positions[i]
+ * away from it, new tokens positions[c] - positions[i]:
+ *     s_j = scale * <q_i, K_g[j]> + alibi_slopes[h] * distance;   out_i = sum_j softmax(s)_j V_g[j]
+ * A token that sees no key is +0.  With prefix_table empty (num_prefix_blocks 0) all of a sequence lies in its own blocks.  New
+ * tokens that lie in the prefix are not seen.
+ *
+ *   tree_masks      [num_tokens][mask_words] uint32: token i's bit c is bit c % 32 of word c / 32; max_q_len at most 32 * mask_words.
+ *                   Bits from n_b on are not looked at; optgqa_tree_masks_host makes masks from parents
+ *   positions       [num_tokens] int32 (in a tree: base + depth); NULL is taken where alibi_slopes is
+ *   workspace       optgqa_tree_workspace_bytes(...) bytes, which grow with each argument as optgqa_common_prefix_workspace_bytes does
+ * All else - q, tables, lengths, slopes, 8-bit caches, what is not finite, bounds, errors - as optgqa_paged_attention_common.
+ */
+size_t optgqa_tree_workspace_bytes(int num_tokens, int num_seqs, int num_heads, int num_kv_heads,
+                                   int head_dim, int block_size, int num_prefix_blocks,
+                                   int max_context_len, int max_q_len);
+
+int optgqa_paged_attention_tree(void *out, const void *q, const void *k_cache, const void *v_cache,
+                                const int32_t *prefix_table, const int32_t *block_tables,
+                                const int32_t *context_lens, const int32_t *cu_q_lens,
+                                const uint32_t *tree_masks, const int32_t *positions,
+                                const float *alibi_slopes, float scale, int mask_words,
+                                int num_tokens, int num_seqs, int num_heads, int num_kv_heads,
+                                int head_dim, int block_size, int num_prefix_blocks,
+                                int max_blocks_per_seq, int max_context_len, int max_q_len,
+                                void *workspace, size_t workspace_bytes, int dtype,
+                                void *stream);
+
+int optgqa_paged_attention_tree_fp8(void *out, const void *q, const void *k_cache, const void *v_cache,
+                                    const int32_t *prefix_table, const int32_t *block_tables,
+                                    const int32_t *context_lens, const int32_t *cu_q_lens,
+                                    const uint32_t *tree_masks, const int32_t *positions,
+                                    const float *alibi_slopes, float scale, float k_scale, float v_scale,
+                                    int mask_words,
+                                    int num_tokens, int num_seqs, int num_heads, int num_kv_heads,
+                                    int head_dim, int block_size, int num_prefix_blocks,
+                                    int max_blocks_per_seq, int max_context_len, int max_q_len,
+                                    void *workspace, size_t workspace_bytes, int dtype,
+                                    void *stream);
+
+int optgqa_paged_attention_tree_fp8_heads(void *out, const void *q, const void *k_cache, const void *v_cache,
+                                          const int32_t *prefix_table, const int32_t *block_tables,
+                                          const int32_t *context_lens, const int32_t *cu_q_lens,
+                                          const uint32_t *tree_masks, const int32_t *positions,
+                                          const float *alibi_slopes, float scale, const float *k_scales, const float *v_scales,
+                                          int mask_words,
+                                          int num_tokens, int num_seqs, int num_heads, int num_kv_heads,
+                                          int head_dim, int block_size, int num_prefix_blocks,
+                                          int max_blocks_per_seq, int max_context_len, int max_q_len,
+                                          void *workspace, size_t workspace_bytes, int dtype,
+                                          void *stream);
+
+/*
+ * Masks and depths of a tree's nodes from their parents, on the host: parents_host[i] < i is node i's parent, negative for a root
+ * (OPTGQA_ERR_TABLE for any other).  Node i's mask [mask_words] has its own bit and those of its ancestors; num_nodes at most
+ * 32 * mask_words.
+ */
+int optgqa_tree_masks_host(uint32_t *masks_host, int32_t *depths_host, const int32_t *parents_host,
+                           int num_nodes, int mask_words);
+
+/*
  * Verification of drafted tokens (speculative decoding) from given random numbers.  Sequence b has
  * n_b = cu_draft_lens[b+1] - cu_draft_lens[b] drafts (at most max_drafts are looked at): draft i is token
  * x = draft_tokens[cu_draft_lens[b] + i], drawn from row cu_draft_lens[b] + i of draft_probs (q); the target model's

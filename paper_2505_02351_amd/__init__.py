@@ -820,8 +820,9 @@ def validate_tables_host(block_tables, context_lens, block_size: int, num_blocks
 from . import operators, pages  # noqa: E402  (they use the helpers above)
 from .operators import (  # noqa: E402, F401
     ROTARY_BASE, ROTARY_LINEAR, ROTARY_PLAIN, ROTARY_WAVELENGTH, ROTARY_YARN, common_prefix_workspace_bytes, paged_attention_common,
-    paged_attention_common_fp8, paged_attention_common_fp8_heads, rotary_and_cache, rotary_and_cache_fp8, rotary_and_cache_fp8_heads,
-    rotary_embedding, rotary_frequencies, verify_drafts, verify_drafts_workspace_bytes,
+    paged_attention_common_fp8, paged_attention_common_fp8_heads, paged_attention_tree, paged_attention_tree_fp8,
+    paged_attention_tree_fp8_heads, rotary_and_cache, rotary_and_cache_fp8, rotary_and_cache_fp8_heads, rotary_embedding, rotary_frequencies,
+    tree_masks, tree_workspace_bytes, verify_drafts, verify_drafts_workspace_bytes,
 )
 from .pages import (  # noqa: E402, F401
     CacheSet, compact_blocks, compact_workspace_bytes, copy_blocks, fork_sequences, keep_tokens, resize_sequences, resize_workspace_bytes,

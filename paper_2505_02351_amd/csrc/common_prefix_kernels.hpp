@@ -75,6 +75,10 @@ struct CommonParams {
     float2* ml;                 // per piece [32]: m, l
     PrefixItems p_items;
     FastDiv by_group, by_kv_heads, by_s_shares;
+    // TREE: which of the sequence's new tokens a token sees, bit c of its words for the c-th; tokens' positions (nullptr: no slopes)
+    const uint32_t* masks;      // [T][mask_words]
+    const int32_t* positions;   // [T]
+    int mask_words;
 };
 
 template <int D, bool KV8> constexpr int kCommonLds = [] {
@@ -88,6 +92,7 @@ template <int D, bool KV8> constexpr int kCommonLds = [] {
 struct TokenPlace {
     int seq, len, first, end;
     __device__ __forceinline__ int pos(int t) const { return seq < 0 ? -1 : len - end + t; }
+    __device__ __forceinline__ int base() const { return seq < 0 ? 0 : len - (end - first); }     // keys before its first new token's
 };
 // What the guess needs, asked for here and used by find() (so that other loads can be asked for in between).
 struct PlaceGuess {
@@ -206,7 +211,7 @@ template <int DT> __device__ __forceinline__ uint32_t finite_pair(uint32_t w)
     return w;
 }
 
-template <int DT, bool KV8, int D, int RW>
+template <int DT, bool KV8, int D, bool TREE, int RW>
 __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJob& job)
 {
     constexpr int KS = kCommonWaves / RW;
@@ -238,8 +243,14 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
         for (int m = 0; m < kQ; ++m) qb[m] = *reinterpret_cast<const uint4*>(qp + (KV8 ? 64 * (m >> 1) + 16 * (m & 1) : 32 * m));
     }
     float slope = p.slopes ? p.slopes[head] : 0.f;
-    int pos = job.pos0 + ti;
-    if (job.prefix) pos = PlaceGuess(p, t).find(p, t).pos(t);
+    int pos = job.pos0 + ti;                                     // its position, and the keys that it sees without a look at a mask
+    int sees = TREE ? job.pos0 : pos + 1;
+    if (job.prefix) {
+        const TokenPlace at = PlaceGuess(p, t).find(p, t);
+        pos = at.pos(t);
+        sees = TREE ? at.base() : pos + 1;
+    }
+    if (TREE && p.positions) pos = p.positions[t];
     auto has = [&](int j) __attribute__((always_inline)) { return j * KS + kw < ntiles; };
 
     // ---- where tiles come from: a lane holds one of 64 block numbers -------------------------------------
@@ -318,7 +329,7 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
 #pragma unroll
         for (int j = 0; j < NBUF; ++j) ask_k(j), ask_v(j);
     }
-    const int lim = row_ok ? min(pos + 1, kend) : kend;          // keys below it are visible
+    const int lim = row_ok ? min(sees, kend) : kend;             // keys below it are visible
     const int least = -wave_max(-lim);                           // tiles that end at or below it need no mask
     const uint32_t keep_q = row_ok ? 0xffffffffu : 0u;
 #pragma unroll
@@ -362,6 +373,18 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
         return st;
     };
     uint32_t pk[2][4], pk_lo[2][4];                              // weights as pairs of 2-byte values (and what is left of them)
+    // TREE: which of a tile's 32 keys the row sees.  Of a sequence's own keys those behind its context are its new tokens, whose bits
+    // lie in two words of the row's mask (in front of it all are seen, behind it none).
+    auto visible = [&](int key0) __attribute__((always_inline)) {
+        const int left = (job.prefix ? lim : kend) - key0;
+        const uint32_t there = left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1u;
+        if (job.prefix) return there;
+        const int c0 = key0 - job.pos0, w = c0 >> 5;
+        const uint32_t* const words = p.masks + (int64_t)t * p.mask_words;
+        const uint32_t lo = w < 0 ? 0xffffffffu : w < p.mask_words ? words[w] : 0u;
+        const uint32_t hi = w + 1 < 0 ? 0xffffffffu : w + 1 < p.mask_words ? words[w + 1] : 0u;
+        return __builtin_amdgcn_alignbit(hi, lo, (uint32_t)c0 & 31u) & there;
+    };
     // key0: the tile's first key
     auto softmax = [&](int key0, f32x16 st, auto masked) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(masked)::value;
@@ -370,7 +393,21 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             x[e] = fmaf(st[e], scale2, b0);
-            if (MASKED) x[e] = key0 + 4 * h2 + 8 * (e >> 2) + (e & 3) < lim ? x[e] : -INFINITY;
+            if (MASKED && !TREE) x[e] = key0 + 4 * h2 + 8 * (e >> 2) + (e & 3) < lim ? x[e] : -INFINITY;
+        }
+        if (MASKED && TREE) {
+            const uint32_t mine = visible(key0) >> (4 * h2);
+            if (p.positions && !job.prefix) {                    // new tokens lie where they were put, and count where they are said to be
+                const int last = p.by_group.div(job.num_rows) - 1;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int in_tile = 8 * (e >> 2) + (e & 3), key = key0 + 4 * h2 + in_tile, c = key - job.pos0;
+                    const int said = p.positions[job.tok0 + min(max(c, 0), last)];
+                    x[e] = fmaf(st[e], scale2, fmaf(slope2, (float)((c < 0 ? key : said) - in_tile - pos), -m_ref));
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = mine >> (8 * (e >> 2) + (e & 3)) & 1 ? x[e] : -INFINITY;
         }
         float mx = x[0];
 #pragma unroll
@@ -461,9 +498,10 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
                 const uint4 va = v_operand(at, m, db);
                 acc[db] = weighted(make_uint4(finite_pair<DT>(va.x), finite_pair<DT>(va.y), finite_pair<DT>(va.z), finite_pair<DT>(va.w)), m, acc[db]);
             }
+        const uint32_t seen = TREE ? visible(key0) : 0u;
 #pragma unroll 1
         for (int k = 0; k < kPfKeys; ++k) {
-            const bool sees = key0 + k < lim;
+            const bool sees = TREE ? seen >> k & 1 : key0 + k < lim;
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {                  // dims 8i + 4 h2 .. + 3
                 uint2 v;
@@ -605,7 +643,7 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
     }
 }
 
-template <int DT, bool KV8, int D>
+template <int DT, bool KV8, int D, bool TREE>
 __global__ __launch_bounds__(kCommonThreads, 2) void common_prefix_kernel(const CommonParams p)
 {
     const int lane = threadIdx.x & 63;
@@ -647,18 +685,18 @@ __global__ __launch_bounds__(kCommonThreads, 2) void common_prefix_kernel(const 
         job.g = __builtin_amdgcn_readfirstlane(segment / tiles);
         job.row0 = (segment - job.g * tiles) * 32 * row_waves;
         job.pos0 = len - p.by_group.div(job.num_rows);
-        // to the position of the tile's last row
+        // to the position of the tile's last row (TREE: to the last new token)
         job.kbeg = p.prefix_len + (lo << OwnParts::keys_shift(p));
-        job.kend = min(job.pos0 + p.by_group.div(min(job.row0 + 32 * row_waves, job.num_rows) - 1) + 1, p.prefix_len + (hi << OwnParts::keys_shift(p)));
+        job.kend = min(TREE ? len : job.pos0 + p.by_group.div(min(job.row0 + 32 * row_waves, job.num_rows) - 1) + 1, p.prefix_len + (hi << OwnParts::keys_shift(p)));
         if (job.kend <= job.kbeg) return;                        // (beyond what its rows see; the join knows)
         job.table = p.block_tables + (int64_t)b * p.max_blocks_per_seq;
         job.slot = p.s_first + (int64_t)me * row_waves;
     }
     job.held_first = job.kbeg >> p.block_shift;
     job.held = job.table[min(job.held_first + lane, (job.kend - 1) >> p.block_shift)];
-    if (row_waves == 4) common_body<DT, KV8, D, 4>(p, job);
-    else if (row_waves == 2) common_body<DT, KV8, D, 2>(p, job);
-    else common_body<DT, KV8, D, 1>(p, job);
+    if (row_waves == 4) common_body<DT, KV8, D, TREE, 4>(p, job);
+    else if (row_waves == 2) common_body<DT, KV8, D, TREE, 2>(p, job);
+    else common_body<DT, KV8, D, TREE, 1>(p, job);
 }
 
 // N pieces of a lane's row: i0, i0 + 4, ..; of 8 J of their dims the lane's halves.
@@ -713,7 +751,7 @@ template <int J> struct JoinState {
     }
 };
 // The pieces of 32 rows joined: workgroup (row block x KV head, DIMS dims), the pieces dealt to its four waves.
-template <int DT, int D, int DIMS>
+template <int DT, int D, int DIMS, bool TREE>
 __global__ __launch_bounds__(kCommonThreads) void common_join_kernel(const CommonParams p)
 {
     constexpr int J = DIMS / 8;
@@ -740,7 +778,7 @@ __global__ __launch_bounds__(kCommonThreads) void common_join_kernel(const Commo
     int64_t piece0 = 0;
     if (p.s_shares > 0) {
         const TokenPlace at = guess.find(p, t);
-        const int behind = at.pos(t) + 1 - p.prefix_len;
+        const int behind = (TREE ? at.len : at.pos(t) + 1) - p.prefix_len;        // (no sequence: 0)
         const int share = own_share(p, parts);
         int all = 0;
         for (int from = 0;;) {

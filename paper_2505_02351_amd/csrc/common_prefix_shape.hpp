@@ -49,10 +49,15 @@ struct CommonPlan {
 // Row blocks of a workgroup for so many rows: 1, 2 or 4 of 32.
 inline int common_row_waves(int64_t rows) { return rows > 64 ? 4 : rows > 32 ? 2 : 1; }
 
+// Shares of all own parts: half a workgroup to a CU beside the prefix's; trees with no prefix have the CUs to themselves, two
+// workgroups to each.
+inline int64_t common_most_shares(int64_t cus, bool alone) { return std::max<int64_t>(alone ? 2 * cus : cus / 2, 1); }
+
 // Pieces that any call has that is no larger in its tokens, sequences, prefix, longest context and new tokens of a sequence: what is
 // held for a call serves all smaller ones.  (The pieces of the calls themselves go up and down: a workgroup's worth of rows more
 // means fewer ranges of the prefix.)
-inline int64_t common_held(int64_t rows, int64_t num_seqs, int64_t own_rows, int num_kv_heads, int64_t prefix_len, int64_t max_context_len, int64_t cus)
+inline int64_t common_held(int64_t rows, int64_t num_seqs, int64_t own_rows, int num_kv_heads, int64_t prefix_len, int64_t max_context_len, int64_t cus,
+                           int64_t most_shares)
 {
     int64_t prefix = 0, own = 0;
     if (prefix_len > 0) {
@@ -65,8 +70,8 @@ inline int64_t common_held(int64_t rows, int64_t num_seqs, int64_t own_rows, int
     for (int w = 1; max_context_len > 0 && w <= common_row_waves(own_rows); w *= 2) {
         const int64_t tile_rows = 32 * w, r = w < 4 ? std::min(own_rows, tile_rows) : own_rows;
         const int64_t tiles = std::min(num_seqs * ((r + tile_rows - 1) / tile_rows), rows / tile_rows + num_seqs);
-        const int64_t step = 32 * (kCommonWaves / w), most = std::max<int64_t>(cus / 2, 1);
-        const int64_t shares = std::min(most, std::min(most, num_kv_heads * tiles) * ((max_context_len + step - 1) / step));
+        const int64_t step = 32 * (kCommonWaves / w);
+        const int64_t shares = std::min(most_shares, std::min(most_shares, num_kv_heads * tiles) * ((max_context_len + step - 1) / step));
         own = std::max(own, w * (shares + num_kv_heads * (rows / tile_rows + num_seqs)));
     }
     return prefix + own;
@@ -74,7 +79,7 @@ inline int64_t common_held(int64_t rows, int64_t num_seqs, int64_t own_rows, int
 
 // false: sizes beyond the kernels' 32-bit counts or a launch's workgroups
 inline bool plan_common(CommonPlan& c, int64_t num_tokens, int64_t num_seqs, int num_heads, int num_kv_heads, int64_t prefix_len, int64_t max_context_len,
-                        int64_t max_q_len, int64_t cus)
+                        int64_t max_q_len, int64_t cus, bool tree = false)
 {
     const int64_t group = num_heads / num_kv_heads;
     c = CommonPlan{};
@@ -104,12 +109,12 @@ inline bool plan_common(CommonPlan& c, int64_t num_tokens, int64_t num_seqs, int
         if (each > (1 << 20) || num_kv_heads * tiles >= (1ll << 30) || num_kv_heads * tiles * each >= (1ll << 30)) return false;
         // (a piece of half of all CUs' share: with more pieces, and with fewer, 64 sequences behind 4 096 tokens, own parts of 127 - 1 023, take
         // 37 - 38 us instead of 32, behind 32 768, 1 023 - 2 047, 110 - 125 instead of 110)
-        c.s_shares = (int)std::min<int64_t>(std::max<int64_t>(cus / 2, 1), num_kv_heads * tiles * each);
+        c.s_shares = (int)std::min<int64_t>(common_most_shares(cus, tree && prefix_len == 0), num_kv_heads * tiles * each);
         // no more than the shares and one for each segment
         c.s_workgroups = c.s_shares + num_kv_heads * (c.rows / tile_rows + num_seqs);
     }
     if (c.workgroups() > kCommonMostWorkgroups) return false;
-    c.held = common_held(c.rows, num_seqs, own_rows, num_kv_heads, prefix_len, max_context_len, cus);
+    c.held = common_held(c.rows, num_seqs, own_rows, num_kv_heads, prefix_len, max_context_len, cus, common_most_shares(cus, tree));
     return true;
 }
 

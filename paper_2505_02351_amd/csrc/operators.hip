@@ -1,5 +1,5 @@
 // C ABI of a step of drafted tokens behind a common prompt: rotary positions, rotated cache appends, attention with a prefix that
-// all sequences have in common, the verification of drafts.
+// all sequences have in common, of lines and of trees of new tokens, the verification of drafts.
 // Declarations and the meaning of every argument: include/optgqa.h.
 #include "optgqa.h"
 
@@ -171,34 +171,49 @@ int launch_verify(const VerifyParams& a, int num_seqs, hipStream_t st)
     return rc != OPTGQA_OK ? rc : launch(verify_select_kernel<DT>, dim3(num_seqs), dim3(64), 0, st, a);
 }
 
-template <int DT, bool KV8, int D>
+template <int DT, bool KV8, int D, bool TREE>
 int launch_common(const CommonParams& p, int workgroups, hipStream_t st)
 {
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&common_prefix_kernel<DT, KV8, D>),
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&common_prefix_kernel<DT, KV8, D, TREE>),
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, kCommonLds<D, KV8>);
     if (attr != hipSuccess) return OPTGQA_ERR_LAUNCH;
     if (workgroups > 0) {
-        const int rc = launch(common_prefix_kernel<DT, KV8, D>, dim3(workgroups), dim3(kCommonThreads), kCommonLds<D, KV8>, st, p);
+        const int rc = launch(common_prefix_kernel<DT, KV8, D, TREE>, dim3(workgroups), dim3(kCommonThreads), kCommonLds<D, KV8>, st, p);
         if (rc != OPTGQA_OK) return rc;
     }
     // 32 dims to a workgroup of the join, 16 where those would not be one to a CU (16 sequences of 32 / 8 heads of 128 behind 6 528
     // tokens: 16.0 us against 16.4; 32 of 3 - 6 new tokens each, 40 / 8 heads: 47.1 against 44.9)
     const int tiles = p.p_slots * p.num_kv_heads;
-    return (int64_t)tiles * (D / 32) < num_cus() ? launch(common_join_kernel<DT, D, 16>, dim3(tiles, D / 16), dim3(kCommonThreads), 0, st, p)
-                                                 : launch(common_join_kernel<DT, D, 32>, dim3(tiles, D / 32), dim3(kCommonThreads), 0, st, p);
+    return (int64_t)tiles * (D / 32) < num_cus() ? launch(common_join_kernel<DT, D, 16, TREE>, dim3(tiles, D / 16), dim3(kCommonThreads), 0, st, p)
+                                                 : launch(common_join_kernel<DT, D, 32, TREE>, dim3(tiles, D / 32), dim3(kCommonThreads), 0, st, p);
 }
 
-template <int DT, bool KV8>
+template <int DT, bool KV8, bool TREE>
 int launch_common_d(const CommonParams& p, int head_dim, int workgroups, hipStream_t st)
 {
-    return head_dim == 128 ? launch_common<DT, KV8, 128>(p, workgroups, st) : launch_common<DT, KV8, 64>(p, workgroups, st);
+    return head_dim == 128 ? launch_common<DT, KV8, 128, TREE>(p, workgroups, st) : launch_common<DT, KV8, 64, TREE>(p, workgroups, st);
 }
+
+template <bool TREE>
+int launch_common_t(const CommonParams& p, int dtype, bool kv8, int head_dim, int workgroups, hipStream_t st)
+{
+    if (dtype == OPTGQA_F16)
+        return kv8 ? launch_common_d<kF16, true, TREE>(p, head_dim, workgroups, st) : launch_common_d<kF16, false, TREE>(p, head_dim, workgroups, st);
+    return kv8 ? launch_common_d<kBF16, true, TREE>(p, head_dim, workgroups, st) : launch_common_d<kBF16, false, TREE>(p, head_dim, workgroups, st);
+}
+
+// Which new tokens see which, where that is not those before them.
+struct TreeCall {
+    const uint32_t* masks;
+    const int32_t* positions;
+    int words;
+};
 
 int common_impl(void* out, const void* q, const void* k_cache, const void* v_cache, const int32_t* prefix_table,
                 const int32_t* block_tables, const int32_t* context_lens, const int32_t* cu_q_lens, const float* alibi_slopes, float scale,
                 int num_tokens, int num_seqs, int num_heads, int num_kv_heads, int head_dim, int block_size, int num_prefix_blocks,
                 int max_blocks_per_seq, int max_context_len, int max_q_len, void* workspace, size_t workspace_bytes, int dtype,
-                const KvScales* scales, void* stream)
+                const KvScales* scales, const TreeCall* tree, void* stream)
 {
     if (num_tokens < 0 || num_seqs < 0 || num_heads <= 0 || num_kv_heads <= 0 || head_dim <= 0 || block_size <= 0 || num_prefix_blocks < 0 ||
         max_blocks_per_seq < 0 || max_context_len < 0 || max_q_len < 0)
@@ -210,14 +225,18 @@ int common_impl(void* out, const void* q, const void* k_cache, const void* v_cac
     if (prefix_len > (1ll << 30) || max_context_len > (1 << 30)) return OPTGQA_ERR_SHAPE;
     if (scales && scales->per_head() && !scales->v_heads) return OPTGQA_ERR_NULL;
     if (scales && !scales->valid()) return OPTGQA_ERR_SHAPE;
+    if (tree && (tree->words <= 0 || max_q_len > (int64_t)tree->words * 32)) return OPTGQA_ERR_SHAPE;
     if (num_tokens == 0) return OPTGQA_OK;
     if (num_seqs == 0 || (!cu_q_lens && num_tokens != num_seqs)) return OPTGQA_ERR_SHAPE;
     if (max_q_len == 0) return OPTGQA_ERR_SHAPE;
     if (!out || !q || !k_cache || !v_cache || !context_lens || (num_prefix_blocks && !prefix_table) || (max_context_len > prefix_len && !block_tables))
         return OPTGQA_ERR_NULL;
+    if (tree && (!tree->masks || (alibi_slopes && !tree->positions))) return OPTGQA_ERR_NULL;
+    if (tree && ((reinterpret_cast<uintptr_t>(tree->masks) | reinterpret_cast<uintptr_t>(tree->positions)) & 3u)) return OPTGQA_ERR_UNSUPPORTED;
     if (!aligned16(out) || !aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache)) return OPTGQA_ERR_UNSUPPORTED;
     CommonPlan c;
-    if (!plan_common(c, num_tokens, num_seqs, num_heads, num_kv_heads, prefix_len, max_context_len, cu_q_lens ? max_q_len : 1, num_cus())) return OPTGQA_ERR_SHAPE;
+    if (!plan_common(c, num_tokens, num_seqs, num_heads, num_kv_heads, prefix_len, max_context_len, cu_q_lens ? max_q_len : 1, num_cus(), tree != nullptr))
+        return OPTGQA_ERR_SHAPE;
     if (!workspace || !aligned16(workspace) || workspace_bytes < c.bytes(head_dim)) return OPTGQA_ERR_WORKSPACE;
 
     CommonParams p;
@@ -264,11 +283,29 @@ int common_impl(void* out, const void* q, const void* k_cache, const void* v_cac
     p.by_group.set((uint32_t)p.group);
     p.by_kv_heads.set((uint32_t)num_kv_heads);
     p.by_s_shares.set((uint32_t)std::max(c.s_shares, 1));
+    p.masks = tree ? tree->masks : nullptr;
+    p.positions = tree && alibi_slopes ? tree->positions : nullptr;
+    p.mask_words = tree ? tree->words : 0;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int workgroups = (int)c.workgroups();
-    if (dtype == OPTGQA_F16)
-        return scales ? launch_common_d<kF16, true>(p, head_dim, workgroups, st) : launch_common_d<kF16, false>(p, head_dim, workgroups, st);
-    return scales ? launch_common_d<kBF16, true>(p, head_dim, workgroups, st) : launch_common_d<kBF16, false>(p, head_dim, workgroups, st);
+    return tree ? launch_common_t<true>(p, dtype, scales != nullptr, head_dim, workgroups, st)
+                : launch_common_t<false>(p, dtype, scales != nullptr, head_dim, workgroups, st);
+}
+
+size_t common_bytes(int num_tokens, int num_seqs, int num_heads, int num_kv_heads, int head_dim, int block_size, int num_prefix_blocks,
+                    int max_context_len, int max_q_len, bool tree)
+{
+    if (num_tokens <= 0 || num_seqs <= 0 || num_heads <= 0 || num_heads > 65535 || num_kv_heads <= 0 || num_heads % num_kv_heads || !head_dim_ok(head_dim) ||
+        !block_size_ok(block_size) || num_prefix_blocks < 0 || max_context_len < 0 || max_q_len <= 0)
+        return 0;
+    // (without prefix sums of new tokens a sequence has one, whatever the bound: the call needs the larger of the two)
+    size_t bytes = 16;
+    for (const int n : {max_q_len, 1}) {
+        CommonPlan c;
+        if (!plan_common(c, num_tokens, num_seqs, num_heads, num_kv_heads, (int64_t)num_prefix_blocks * block_size, max_context_len, n, num_cus(), tree)) return 0;
+        bytes = std::max(bytes, c.bytes(head_dim));
+    }
+    return bytes;
 }
 
 }  // namespace
@@ -411,17 +448,7 @@ int optgqa_verify_drafts(int64_t* tokens, int32_t* num_accepted, const void* tar
 size_t optgqa_common_prefix_workspace_bytes(int num_tokens, int num_seqs, int num_heads, int num_kv_heads, int head_dim,
                                             int block_size, int num_prefix_blocks, int max_context_len, int max_q_len)
 {
-    if (num_tokens <= 0 || num_seqs <= 0 || num_heads <= 0 || num_heads > 65535 || num_kv_heads <= 0 || num_heads % num_kv_heads || !head_dim_ok(head_dim) ||
-        !block_size_ok(block_size) || num_prefix_blocks < 0 || max_context_len < 0 || max_q_len <= 0)
-        return 0;
-    // (without prefix sums of new tokens a sequence has one, whatever the bound: the call needs the larger of the two)
-    size_t bytes = 16;
-    for (const int n : {max_q_len, 1}) {
-        CommonPlan c;
-        if (!plan_common(c, num_tokens, num_seqs, num_heads, num_kv_heads, (int64_t)num_prefix_blocks * block_size, max_context_len, n, num_cus())) return 0;
-        bytes = std::max(bytes, c.bytes(head_dim));
-    }
-    return bytes;
+    return common_bytes(num_tokens, num_seqs, num_heads, num_kv_heads, head_dim, block_size, num_prefix_blocks, max_context_len, max_q_len, false);
 }
 
 int optgqa_paged_attention_common(void* out, const void* q, const void* k_cache, const void* v_cache, const int32_t* prefix_table,
@@ -432,7 +459,7 @@ int optgqa_paged_attention_common(void* out, const void* q, const void* k_cache,
 {
     return common_impl(out, q, k_cache, v_cache, prefix_table, block_tables, context_lens, cu_q_lens, alibi_slopes, scale, num_tokens, num_seqs,
                        num_heads, num_kv_heads, head_dim, block_size, num_prefix_blocks, max_blocks_per_seq, max_context_len, max_q_len, workspace,
-                       workspace_bytes, dtype, nullptr, stream);
+                       workspace_bytes, dtype, nullptr, nullptr, stream);
 }
 
 int optgqa_paged_attention_common_fp8(void* out, const void* q, const void* k_cache, const void* v_cache, const int32_t* prefix_table,
@@ -444,7 +471,7 @@ int optgqa_paged_attention_common_fp8(void* out, const void* q, const void* k_ca
     const KvScales scales{k_scale, v_scale, nullptr, nullptr};
     return common_impl(out, q, k_cache, v_cache, prefix_table, block_tables, context_lens, cu_q_lens, alibi_slopes, scale, num_tokens, num_seqs,
                        num_heads, num_kv_heads, head_dim, block_size, num_prefix_blocks, max_blocks_per_seq, max_context_len, max_q_len, workspace,
-                       workspace_bytes, dtype, &scales, stream);
+                       workspace_bytes, dtype, &scales, nullptr, stream);
 }
 
 int optgqa_paged_attention_common_fp8_heads(void* out, const void* q, const void* k_cache, const void* v_cache, const int32_t* prefix_table,
@@ -457,7 +484,72 @@ int optgqa_paged_attention_common_fp8_heads(void* out, const void* q, const void
     const KvScales scales{0.f, 0.f, k_scales, v_scales};
     return common_impl(out, q, k_cache, v_cache, prefix_table, block_tables, context_lens, cu_q_lens, alibi_slopes, scale, num_tokens, num_seqs,
                        num_heads, num_kv_heads, head_dim, block_size, num_prefix_blocks, max_blocks_per_seq, max_context_len, max_q_len, workspace,
-                       workspace_bytes, dtype, &scales, stream);
+                       workspace_bytes, dtype, &scales, nullptr, stream);
+}
+
+size_t optgqa_tree_workspace_bytes(int num_tokens, int num_seqs, int num_heads, int num_kv_heads, int head_dim, int block_size,
+                                   int num_prefix_blocks, int max_context_len, int max_q_len)
+{
+    return common_bytes(num_tokens, num_seqs, num_heads, num_kv_heads, head_dim, block_size, num_prefix_blocks, max_context_len, max_q_len, true);
+}
+
+int optgqa_paged_attention_tree(void* out, const void* q, const void* k_cache, const void* v_cache, const int32_t* prefix_table,
+                                const int32_t* block_tables, const int32_t* context_lens, const int32_t* cu_q_lens, const uint32_t* tree_masks,
+                                const int32_t* positions, const float* alibi_slopes, float scale, int mask_words, int num_tokens,
+                                int num_seqs, int num_heads, int num_kv_heads, int head_dim, int block_size, int num_prefix_blocks,
+                                int max_blocks_per_seq, int max_context_len, int max_q_len, void* workspace, size_t workspace_bytes,
+                                int dtype, void* stream)
+{
+    const TreeCall tree{tree_masks, positions, mask_words};
+    return common_impl(out, q, k_cache, v_cache, prefix_table, block_tables, context_lens, cu_q_lens, alibi_slopes, scale, num_tokens, num_seqs,
+                       num_heads, num_kv_heads, head_dim, block_size, num_prefix_blocks, max_blocks_per_seq, max_context_len, max_q_len, workspace,
+                       workspace_bytes, dtype, nullptr, &tree, stream);
+}
+
+int optgqa_paged_attention_tree_fp8(void* out, const void* q, const void* k_cache, const void* v_cache, const int32_t* prefix_table,
+                                const int32_t* block_tables, const int32_t* context_lens, const int32_t* cu_q_lens, const uint32_t* tree_masks,
+                                const int32_t* positions, const float* alibi_slopes, float scale, float k_scale, float v_scale, int mask_words, int num_tokens,
+                                int num_seqs, int num_heads, int num_kv_heads, int head_dim, int block_size, int num_prefix_blocks,
+                                int max_blocks_per_seq, int max_context_len, int max_q_len, void* workspace, size_t workspace_bytes,
+                                int dtype, void* stream)
+{
+    const KvScales scales{k_scale, v_scale, nullptr, nullptr};
+    const TreeCall tree{tree_masks, positions, mask_words};
+    return common_impl(out, q, k_cache, v_cache, prefix_table, block_tables, context_lens, cu_q_lens, alibi_slopes, scale, num_tokens, num_seqs,
+                       num_heads, num_kv_heads, head_dim, block_size, num_prefix_blocks, max_blocks_per_seq, max_context_len, max_q_len, workspace,
+                       workspace_bytes, dtype, &scales, &tree, stream);
+}
+
+int optgqa_paged_attention_tree_fp8_heads(void* out, const void* q, const void* k_cache, const void* v_cache, const int32_t* prefix_table,
+                                const int32_t* block_tables, const int32_t* context_lens, const int32_t* cu_q_lens, const uint32_t* tree_masks,
+                                const int32_t* positions, const float* alibi_slopes, float scale, const float* k_scales, const float* v_scales, int mask_words, int num_tokens,
+                                int num_seqs, int num_heads, int num_kv_heads, int head_dim, int block_size, int num_prefix_blocks,
+                                int max_blocks_per_seq, int max_context_len, int max_q_len, void* workspace, size_t workspace_bytes,
+                                int dtype, void* stream)
+{
+    if (!k_scales || !v_scales) return OPTGQA_ERR_NULL;
+    const KvScales scales{0.f, 0.f, k_scales, v_scales};
+    const TreeCall tree{tree_masks, positions, mask_words};
+    return common_impl(out, q, k_cache, v_cache, prefix_table, block_tables, context_lens, cu_q_lens, alibi_slopes, scale, num_tokens, num_seqs,
+                       num_heads, num_kv_heads, head_dim, block_size, num_prefix_blocks, max_blocks_per_seq, max_context_len, max_q_len, workspace,
+                       workspace_bytes, dtype, &scales, &tree, stream);
+}
+
+int optgqa_tree_masks_host(uint32_t* masks_host, int32_t* depths_host, const int32_t* parents_host, int num_nodes, int mask_words)
+{
+    if (num_nodes < 0 || mask_words <= 0 || num_nodes > (int64_t)mask_words * 32) return OPTGQA_ERR_SHAPE;
+    if (num_nodes == 0) return OPTGQA_OK;
+    if (!masks_host || !depths_host || !parents_host) return OPTGQA_ERR_NULL;
+    for (int i = 0; i < num_nodes; ++i)
+        if (parents_host[i] >= i) return OPTGQA_ERR_TABLE;
+    for (int i = 0; i < num_nodes; ++i) {
+        const int parent = parents_host[i];
+        uint32_t* const mine = masks_host + (size_t)i * mask_words;
+        for (int w = 0; w < mask_words; ++w) mine[w] = parent < 0 ? 0u : masks_host[(size_t)parent * mask_words + w];
+        mine[i / 32] |= 1u << (i % 32);
+        depths_host[i] = parent < 0 ? 0 : depths_host[parent] + 1;
+    }
+    return OPTGQA_OK;
 }
 
 }  // extern "C"

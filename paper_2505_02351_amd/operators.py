@@ -1,5 +1,5 @@
 """Binding of the calls that stand around the attention of a step: rotary positions, rotated cache appends, the
-attention of a batch with a common prefix and the verification of drafted tokens.
+attention of a batch with a common prefix and of trees of new tokens, and the verification of drafted tokens.
 
 Conventions as in the package: q [T, Hq, D], k and v [T, Hkv, D] with any token stride (dense in their
 last two dims: slices of one projection's rows will do), caches [NB, Hkv, bs, D], positions [T] int32,
@@ -30,11 +30,15 @@ def declare(lib: ctypes.CDLL) -> None:
         "paged_attention_common": [vp] * 9 + [f32] + [i32] * 10 + [vp, ctypes.c_size_t, i32, vp],
         "paged_attention_common_fp8": [vp] * 9 + [f32] * 3 + [i32] * 10 + [vp, ctypes.c_size_t, i32, vp],
         "paged_attention_common_fp8_heads": [vp] * 9 + [f32, vp, vp] + [i32] * 10 + [vp, ctypes.c_size_t, i32, vp],
+        "paged_attention_tree": [vp] * 11 + [f32] + [i32] * 11 + [vp, ctypes.c_size_t, i32, vp],
+        "paged_attention_tree_fp8": [vp] * 11 + [f32] * 3 + [i32] * 11 + [vp, ctypes.c_size_t, i32, vp],
+        "paged_attention_tree_fp8_heads": [vp] * 11 + [f32, vp, vp] + [i32] * 11 + [vp, ctypes.c_size_t, i32, vp],
+        "tree_masks_host": [vp] * 3 + [i32] * 2,
         "verify_drafts": [vp] * 8 + [i32] * 3 + [i64, i64, vp, ctypes.c_size_t, i32, vp],
     }.items():
         f = getattr(lib, "optgqa_" + name)
         f.restype, f.argtypes = i32, args
-    for name, n in (("common_prefix_workspace_bytes", 9), ("verify_drafts_workspace_bytes", 2)):
+    for name, n in (("common_prefix_workspace_bytes", 9), ("tree_workspace_bytes", 9), ("verify_drafts_workspace_bytes", 2)):
         f = getattr(lib, "optgqa_" + name)
         f.restype, f.argtypes = ctypes.c_size_t, [i32] * n
 
@@ -192,7 +196,8 @@ def common_prefix_workspace_bytes(num_tokens: int, num_seqs: int, num_heads: int
 
 
 def _common(name, out, q, k_cache, v_cache, prefix_table, block_tables, context_lens, cu_q_lens, alibi_slopes, scale, max_context_len,
-            max_q_len, workspace, stream, kv8, scales) -> None:
+            max_q_len, workspace, stream, kv8, scales, tree=()) -> None:
+    """tree: () or (tree_masks, positions or None)."""
     lib = _pkg.load_library()
     code, dtype = _pkg._dtype_code(q), q.dtype
     cache, i32 = torch.uint8 if kv8 else dtype, torch.int32
@@ -200,6 +205,8 @@ def _common(name, out, q, k_cache, v_cache, prefix_table, block_tables, context_
     more = () if cu_q_lens is None else ((cu_q_lens, "cu_q_lens", i32),)
     if alibi_slopes is not None:
         more += ((alibi_slopes, "alibi_slopes", torch.float32),)
+    if tree:
+        more += ((tree[0], "tree_masks", i32),) if tree[1] is None else ((tree[0], "tree_masks", i32), (tree[1], "positions", i32))
     _check_tensors(index, ((q, "q", dtype), (out, "out", dtype), (k_cache, "k_cache", cache), (v_cache, "v_cache", cache),
                            (prefix_table, "prefix_table", i32), (block_tables, "block_tables", i32), (context_lens, "context_lens", i32), *more))
     shape, tables = k_cache.shape, block_tables.shape
@@ -215,10 +222,19 @@ def _common(name, out, q, k_cache, v_cache, prefix_table, block_tables, context_
         _dense((cu_q_lens, "cu_q_lens"))
     if alibi_slopes is not None:
         _dense((alibi_slopes, "alibi_slopes"))
+    masks = words = ()
+    if tree:
+        shape = tree[0].shape
+        if len(shape) != 2 or shape[0] != T or (tree[1] is not None and tree[1].shape != (T,)):
+            raise ValueError("optgqa: shape mismatch between q, tree_masks and positions")
+        _dense(*((t, name) for t, name in zip(tree, ("tree_masks", "positions")) if t is not None))
+        if torch._C._cuda_getDevice() != index:
+            raise ValueError(f"optgqa: the tensors are on GPU {index}, which is not the current one")
+        masks, words = (tree[0].data_ptr(), _pkg._ptr(tree[1])), (shape[1],)
     ws_bytes = _pkg._workspace(workspace, q)
     rc = getattr(lib, name)(out.data_ptr(), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), prefix_table.data_ptr(),
-                            block_tables.data_ptr(), context_lens.data_ptr(), _pkg._ptr(cu_q_lens), _pkg._ptr(alibi_slopes), scale, *scales,
-                            T, B, Hq, Hkv, D, bs, prefix_table.shape[0], tables[1], max_context_len, max_q_len,
+                            block_tables.data_ptr(), context_lens.data_ptr(), _pkg._ptr(cu_q_lens), *masks, _pkg._ptr(alibi_slopes), scale, *scales,
+                            *words, T, B, Hq, Hkv, D, bs, prefix_table.shape[0], tables[1], max_context_len, max_q_len,
                             _pkg._ptr(workspace), ws_bytes, code, _pkg._stream(stream))
     if rc:
         _pkg._check(rc, name)
@@ -252,6 +268,59 @@ def paged_attention_common_fp8_heads(out: torch.Tensor, q: torch.Tensor, k_cache
     _pkg._head_scales(q, k_cache, k_scales, v_scales)
     _common("optgqa_paged_attention_common_fp8_heads", out, q, k_cache, v_cache, prefix_table, block_tables, context_lens, cu_q_lens,
             alibi_slopes, scale, max_context_len, max_q_len, workspace, stream, True, (k_scales.data_ptr(), v_scales.data_ptr()))
+
+
+def tree_workspace_bytes(num_tokens: int, num_seqs: int, num_heads: int, num_kv_heads: int, head_dim: int, block_size: int,
+                         num_prefix_blocks: int, max_context_len: int, max_q_len: int) -> int:
+    """optgqa_tree_workspace_bytes: sized for the largest of each argument, a workspace serves every call."""
+    return int(_pkg.load_library().optgqa_tree_workspace_bytes(num_tokens, num_seqs, num_heads, num_kv_heads, head_dim, block_size,
+                                                               num_prefix_blocks, max_context_len, max_q_len))
+
+
+def tree_masks(parents, mask_words: Optional[int] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """optgqa_tree_masks_host -> (masks [n, mask_words] int32, depths [n] int32) on the CPU, of a tree of n nodes: parents[i] < i, negative
+    for a root.  mask_words: as many as n bits take, unless given."""
+    parents = torch.as_tensor(parents, dtype=torch.int32, device="cpu").contiguous()
+    if len(parents.shape) != 1:
+        raise ValueError("optgqa: parents must have one dimension")
+    n = parents.shape[0]
+    words = max((n + 31) // 32, 1) if mask_words is None else int(mask_words)
+    masks, depths = torch.zeros(n, max(words, 0), dtype=torch.int32), torch.zeros(n, dtype=torch.int32)
+    _pkg._check(_pkg.load_library().optgqa_tree_masks_host(masks.data_ptr(), depths.data_ptr(), parents.data_ptr(), n, words), "optgqa_tree_masks_host")
+    return masks, depths
+
+
+def paged_attention_tree(out: torch.Tensor, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, prefix_table: torch.Tensor,
+                         block_tables: torch.Tensor, context_lens: torch.Tensor, cu_q_lens: Optional[torch.Tensor], tree_masks: torch.Tensor,
+                         positions: Optional[torch.Tensor], alibi_slopes: Optional[torch.Tensor], scale: float, max_context_len: int,
+                         max_q_len: int, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """optgqa_paged_attention_tree: paged_attention_common for trees of new tokens (prefix_table may be empty): each sees the keys
+    before its sequence's new tokens, and of those the ones whose bits are set in its row of tree_masks [T, words] int32;
+    positions [T] int32 (or None, without slopes): where they stand for the slopes."""
+    _common("optgqa_paged_attention_tree", out, q, k_cache, v_cache, prefix_table, block_tables, context_lens, cu_q_lens, alibi_slopes,
+            scale, max_context_len, max_q_len, workspace, stream, False, (), (tree_masks, positions))
+
+
+def paged_attention_tree_fp8(out: torch.Tensor, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, prefix_table: torch.Tensor,
+                             block_tables: torch.Tensor, context_lens: torch.Tensor, cu_q_lens: Optional[torch.Tensor],
+                             tree_masks: torch.Tensor, positions: Optional[torch.Tensor], alibi_slopes: Optional[torch.Tensor], scale: float,
+                             k_scale: float, v_scale: float, max_context_len: int, max_q_len: int, workspace: Optional[torch.Tensor] = None,
+                             stream=None) -> None:
+    """optgqa_paged_attention_tree_fp8: the same over E4M3 caches (uint8 tensors), one scale per tensor."""
+    _common("optgqa_paged_attention_tree_fp8", out, q, k_cache, v_cache, prefix_table, block_tables, context_lens, cu_q_lens, alibi_slopes,
+            scale, max_context_len, max_q_len, workspace, stream, True, (float(k_scale), float(v_scale)), (tree_masks, positions))
+
+
+def paged_attention_tree_fp8_heads(out: torch.Tensor, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                                   prefix_table: torch.Tensor, block_tables: torch.Tensor, context_lens: torch.Tensor,
+                                   cu_q_lens: Optional[torch.Tensor], tree_masks: torch.Tensor, positions: Optional[torch.Tensor],
+                                   alibi_slopes: Optional[torch.Tensor], scale: float, k_scales: torch.Tensor, v_scales: torch.Tensor,
+                                   max_context_len: int, max_q_len: int, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """optgqa_paged_attention_tree_fp8_heads: the same with one scale pair per KV head (float32 device tensors [Hkv])."""
+    _pkg._head_scales(q, k_cache, k_scales, v_scales)
+    _common("optgqa_paged_attention_tree_fp8_heads", out, q, k_cache, v_cache, prefix_table, block_tables, context_lens, cu_q_lens,
+            alibi_slopes, scale, max_context_len, max_q_len, workspace, stream, True, (k_scales.data_ptr(), v_scales.data_ptr()),
+            (tree_masks, positions))
 
 
 _PROBABILITIES = {torch.float16: _pkg.F16, torch.bfloat16: _pkg.BF16, torch.float32: 2}
