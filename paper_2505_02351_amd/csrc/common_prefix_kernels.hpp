@@ -127,13 +127,19 @@ struct PlaceGuess {
     }
 };
 
-// Own parts of 64 sequences, one a lane.  A segment: one KV head, one row tile.
-struct OwnParts {
+// Own parts of 64 sequences, one a lane.  A segment: one KV head, one row tile.  TREE: as many row blocks to a workgroup as the
+// sequence's rows need, up to the launch's.
+template <bool TREE> struct OwnParts {
     int len, first, rows;       // context length, first token, rows (new tokens x heads of the group)
     int steps, segments;        // of a segment; segments (0: nothing to do)
     int pieces, before;         // of a segment; pieces of all sequences before this one (number())
-    static __device__ __forceinline__ int keys_shift(const CommonParams& p) { return 7 - (p.s_row_waves >> 1); }       // a step's: 128, 64, 32 for 1, 2, 4
-    static __device__ __forceinline__ int steps_of(const CommonParams& p, int keys) { return (keys + (1 << keys_shift(p)) - 1) >> keys_shift(p); }
+    int row_waves;              // row blocks to a workgroup: 1, 2 or 4
+    static __device__ __forceinline__ int row_waves_of(const CommonParams& p, int rows)
+    {
+        return TREE ? min(rows > 64 ? 4 : rows > 32 ? 2 : 1, p.s_row_waves) : p.s_row_waves;
+    }
+    static __device__ __forceinline__ int keys_shift(int row_waves) { return 7 - (row_waves >> 1); }                   // a step's: 128, 64, 32 for 1, 2, 4
+    static __device__ __forceinline__ int steps_of(int row_waves, int keys) { return (keys + (1 << keys_shift(row_waves)) - 1) >> keys_shift(row_waves); }
     // those from number `from` on
     __device__ __forceinline__ OwnParts(const CommonParams& p, int from)
     {
@@ -142,8 +148,9 @@ struct OwnParts {
         first = p.cu_q_lens ? p.cu_q_lens[b] : b;
         rows = (p.cu_q_lens ? p.cu_q_lens[b + 1] - first : 1) * p.group;
         const int behind = from + lane < p.num_seqs && rows > 0 ? max(len - p.prefix_len, 0) : 0;
-        steps = steps_of(p, behind);
-        segments = behind > 0 ? ((rows + 32 * p.s_row_waves - 1) >> (4 + 32 - __builtin_clz(p.s_row_waves))) * p.num_kv_heads : 0;
+        row_waves = row_waves_of(p, rows);
+        steps = steps_of(row_waves, behind);
+        segments = behind > 0 ? ((rows + 32 * row_waves - 1) >> (4 + 32 - __builtin_clz(row_waves))) * p.num_kv_heads : 0;
     }
     // a segment has as many equal pieces as shares of `most` steps take; `all`: pieces before these sequences, and then with them
     __device__ __forceinline__ void number(int most, int& all)
@@ -157,11 +164,11 @@ struct OwnParts {
     static __device__ __forceinline__ int each(int steps, int pieces) { return div_by_inverse(steps + pieces - 1, pieces, __builtin_amdgcn_rcpf((float)pieces)); }
 };
 // The most steps of a piece.  `parts`: the first 64 sequences'.
-__device__ __forceinline__ int own_share(const CommonParams& p, const OwnParts& parts)
+template <bool TREE> __device__ __forceinline__ int own_share(const CommonParams& p, const OwnParts<TREE>& parts)
 {
     int total = wave_sum(parts.steps * parts.segments);
     for (int from = 64; from < p.num_seqs; from += 64) {
-        const OwnParts more(p, from);
+        const OwnParts<TREE> more(p, from);
         total += wave_sum(more.steps * more.segments);
     }
     return max(p.by_s_shares.div(total + p.s_shares - 1), 1);
@@ -224,6 +231,7 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
     constexpr int kWaveKeys = kWaveGroups * Tile::kRows;
     constexpr int kHalves = kWaveKeys > 16 ? 2 : 1;              // runs of up to 16 keys, each in one block, they lie in
     constexpr int kRunGroups = kWaveGroups / kHalves;
+    constexpr bool kOneTile = RW == 1 || (TREE && RW == 2);      // no other row tile reads the keys (fewer row blocks than 4: as many as the rows need)
     extern __shared__ __attribute__((aligned(16))) unsigned char common_lds[];
     unsigned char* const lds = common_lds;
     const int lane = threadIdx.x & 63, n32 = lane & 31, h2 = lane >> 5;
@@ -300,7 +308,7 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
 #pragma unroll
         for (int n = 0; n < kWaveGroups; ++n) {
             const uint32_t to = lds0 + at + (first_group + n) * Tile::kGroup;
-            if (RW == 1) stream_direct(to, cache + r.at[n / kRunGroups], r.lane_at[n]);      // (no other row tile reads them)
+            if (kOneTile) stream_direct(to, cache + r.at[n / kRunGroups], r.lane_at[n]);
             else load_direct(to, cache + r.at[n / kRunGroups], r.lane_at[n]);
         }
     };
@@ -318,6 +326,25 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
     };
     auto ask_v = [&](int j) __attribute__((always_inline)) {
         if (has(j) && first_v >= 0) ask(runs_of(j, first_v), vc, buffer_v(j), first_v);
+    };
+    // The same for tiles that end before kend, of waves that bring the same rows of K and V: nothing is clamped, and a V tile lies where the
+    // K tile lay that was asked for a step before (`at`).  (TREE: some 50 instructions a step less, of 270 that one wave to a SIMD works through
+    // one after another: a tile of 32 keys and 128 rows 0.78 -> 0.67 us over E4M3 caches, two workgroups' 1.43 -> 1.27 in bf16.)
+    struct At { uint64_t run[kHalves]; };
+    auto at_of = [&](int j) __attribute__((always_inline)) {
+        At at;
+        const int key0 = kbeg + kPfKeys * (j * KS + kw) + first_k * Tile::kRows;
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) at.run[h] = key_at(key0 + 16 * h);
+        return at;
+    };
+    auto ask_at = [&](const At& at, const unsigned char* cache, int to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < kWaveGroups; ++n) {
+            const uint32_t at_lds = lds0 + to + (first_k + n) * Tile::kGroup;
+            if (kOneTile) stream_direct(at_lds, cache + at.run[n / kRunGroups], lane_off + (n % kRunGroups) * 1024);
+            else load_direct(at_lds, cache + at.run[n / kRunGroups], lane_off + (n % kRunGroups) * 1024);
+        }
     };
     asm volatile("" : "+v"(held) :: "memory");
     if constexpr (RW > 1) {
@@ -534,13 +561,19 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
     const int mine = (ntiles - kw + KS - 1) / KS;                // tiles of this wave's key group
     const int whole = min(mine, max(0, (least - kbeg) / kPfKeys - kw + KS - 1) / KS);
     if constexpr (RW > 1) {
-        auto step = [&](int j, const f32x16& st_cur, f32x16& st_ahead, auto masked) __attribute__((always_inline)) {
+        At at_last;                                              // of the K tile that was asked for last (inner steps)
+        auto step = [&](int j, const f32x16& st_cur, f32x16& st_ahead, auto masked, auto inner) __attribute__((always_inline)) {
             // K tile j + 1 and V tile j are there; newer: step j - 1's, where it asked for all of its own
-            if (kLead > 1 && j + kLead < mine) wait_direct<(kLead - 1) * kLoads>();
+            if (kLead > 1 && (decltype(inner)::value || j + kLead < mine)) wait_direct<(kLead - 1) * kLoads>();
             else wait_direct();
             __syncthreads();                                     // ... for all; and the buffers read in step j - 1 are free
             st_ahead = scores(buffer(j + 1), [&]() __attribute__((always_inline)) {
-                if (j + kLead < mine) {
+                if (decltype(inner)::value) {
+                    const At at = at_of(j + 1 + kLead);
+                    ask_at(at, kc, buffer(j + 1 + kLead));
+                    ask_at(at_last, vc, buffer_v(j + kLead));
+                    at_last = at;
+                } else if (j + kLead < mine) {
                     ask_k(j + 1 + kLead);
                     ask_v(j + kLead);
                 }
@@ -553,17 +586,26 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
         __syncthreads();
         st = scores(buffer(0), [] {});
         int j = 0;
+        if constexpr (TREE && !kHalfLoad) {
+            // steps that need no mask and ask for tiles that are there in full
+            const int full = max((kend - kbeg) / kPfKeys - kw + KS - 1, 0) / KS, inner = min(whole, full - 1 - kLead);
+            if (j + 1 < inner) at_last = at_of(kLead);
+            for (; j + 1 < inner; j += 2) {
+                step(j, st, st_other, std::false_type{}, std::true_type{});
+                step(j + 1, st_other, st, std::false_type{}, std::true_type{});
+            }
+        }
         for (; j + 1 < whole; j += 2) {
-            step(j, st, st_other, std::false_type{});
-            step(j + 1, st_other, st, std::false_type{});
+            step(j, st, st_other, std::false_type{}, std::false_type{});
+            step(j + 1, st_other, st, std::false_type{}, std::false_type{});
         }
         if (j < whole) {
-            step(j, st, st_other, std::false_type{});
+            step(j, st, st_other, std::false_type{}, std::false_type{});
             st = st_other;
             ++j;
         }
         for (; j < steps; ++j) {
-            step(j, st, st_other, std::true_type{});
+            step(j, st, st_other, std::true_type{}, std::false_type{});
             st = st_other;
         }
     } else {
@@ -650,7 +692,7 @@ __global__ __launch_bounds__(kCommonThreads, 2) void common_prefix_kernel(const 
     CommonJob job;
     const int p_workgroups = p.p_items.workgroups();
     job.prefix = (int)blockIdx.x < p_workgroups;
-    const int row_waves = job.prefix ? p.p_row_waves : p.s_row_waves;
+    int row_waves = job.prefix ? p.p_row_waves : p.s_row_waves;
     if (job.prefix) {
         int range, tile;
         if (!p.p_items.place(blockIdx.x, p.p_splits, p.p_tiles, job.g, range, tile)) return;
@@ -663,20 +705,22 @@ __global__ __launch_bounds__(kCommonThreads, 2) void common_prefix_kernel(const 
         job.slot = ((int64_t)range * p.num_kv_heads + job.g) * p.p_slots + tile * row_waves;
     } else {
         const int me = blockIdx.x - p_workgroups;              // the piece
-        OwnParts parts(p, 0);
+        typedef OwnParts<TREE> Own;
+        Own parts(p, 0);
         const int share = own_share(p, parts);
         int all = 0, from = 0;
         parts.number(share, all);
         while (all <= me) {                                      // not one of these sequences'
             from += 64;
             if (from >= p.num_seqs) return;                      // (nobody's)
-            parts = OwnParts(p, from);
+            parts = Own(p, from);
             parts.number(share, all);
         }
         const int l = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(parts.segments > 0 && parts.before <= me));
         const int b = from + l, len = __builtin_amdgcn_readlane(parts.len, l), steps = __builtin_amdgcn_readlane(parts.steps, l);
         const int pieces = __builtin_amdgcn_readlane(parts.pieces, l), in_seq = me - __builtin_amdgcn_readlane(parts.before, l);
-        const int segment = __builtin_amdgcn_readfirstlane(in_seq / pieces), each = __builtin_amdgcn_readfirstlane(OwnParts::each(steps, pieces));
+        const int segment = __builtin_amdgcn_readfirstlane(in_seq / pieces), each = __builtin_amdgcn_readfirstlane(Own::each(steps, pieces));
+        if (TREE) row_waves = __builtin_amdgcn_readlane(parts.row_waves, l);
         const int lo = (in_seq - segment * pieces) * each, hi = min(lo + each, steps);
         if (hi <= lo) return;                                    // (equal pieces of, say, 7 steps in 4: the last is empty)
         job.num_rows = __builtin_amdgcn_readlane(parts.rows, l);
@@ -686,11 +730,11 @@ __global__ __launch_bounds__(kCommonThreads, 2) void common_prefix_kernel(const 
         job.row0 = (segment - job.g * tiles) * 32 * row_waves;
         job.pos0 = len - p.by_group.div(job.num_rows);
         // to the position of the tile's last row (TREE: to the last new token)
-        job.kbeg = p.prefix_len + (lo << OwnParts::keys_shift(p));
-        job.kend = min(TREE ? len : job.pos0 + p.by_group.div(min(job.row0 + 32 * row_waves, job.num_rows) - 1) + 1, p.prefix_len + (hi << OwnParts::keys_shift(p)));
+        job.kbeg = p.prefix_len + (lo << Own::keys_shift(row_waves));
+        job.kend = min(TREE ? len : job.pos0 + p.by_group.div(min(job.row0 + 32 * row_waves, job.num_rows) - 1) + 1, p.prefix_len + (hi << Own::keys_shift(row_waves)));
         if (job.kend <= job.kbeg) return;                        // (beyond what its rows see; the join knows)
         job.table = p.block_tables + (int64_t)b * p.max_blocks_per_seq;
-        job.slot = p.s_first + (int64_t)me * row_waves;
+        job.slot = p.s_first + (int64_t)me * p.s_row_waves;
     }
     job.held_first = job.kbeg >> p.block_shift;
     job.held = job.table[min(job.held_first + lane, (job.kend - 1) >> p.block_shift)];
@@ -762,7 +806,8 @@ __global__ __launch_bounds__(kCommonThreads) void common_join_kernel(const Commo
     const int tile = p.by_kv_heads.div(blockIdx.x), g = blockIdx.x - tile * p.num_kv_heads, part = blockIdx.y;
     const int r = 32 * tile + n32, rc = min(r, p.rows - 1), t = p.by_group.div(rc), head = g * p.group + (rc - t * p.group);
     const PlaceGuess guess(p, t);
-    OwnParts parts(p, 0);
+    typedef OwnParts<TREE> Own;
+    Own parts(p, 0);
     JoinState<J> state;
     const float4* const o = p.o + part * J * 64 + n32 + 32 * h2;
     // the prefix's pieces are there for every row, whatever it sees (m = -inf: nothing): those of a wave, four at a time, the
@@ -786,16 +831,17 @@ __global__ __launch_bounds__(kCommonThreads) void common_join_kernel(const Commo
             const int l = at.seq - from;                         // (all lanes exchange)
             const int before = __shfl(parts.before, l & 63), pieces = __shfl(parts.pieces, l & 63), steps = __shfl(parts.steps, l & 63);
             if (behind > 0 && l >= 0 && l < 64) {
-                const int in_seq = rc - at.first * p.group, tile_rows = 32 * p.s_row_waves, tile_shift = 31 - __builtin_clz(tile_rows);
+                const int waves = Own::row_waves_of(p, (at.end - at.first) * p.group);
+                const int in_seq = rc - at.first * p.group, tile_rows = 32 * waves, tile_shift = 31 - __builtin_clz(tile_rows);
                 const int tiles = ((at.end - at.first) * p.group + tile_rows - 1) >> tile_shift;
-                const int each = OwnParts::each(steps, pieces);
-                n = div_by_inverse(OwnParts::steps_of(p, behind) + each - 1, each, __builtin_amdgcn_rcpf((float)each));
+                const int each = Own::each(steps, pieces);
+                n = div_by_inverse(Own::steps_of(waves, behind) + each - 1, each, __builtin_amdgcn_rcpf((float)each));
                 row_off = (in_seq & 31) - n32;
-                piece0 = p.s_first + (int64_t)(before + (g * tiles + (in_seq >> tile_shift)) * pieces) * p.s_row_waves + ((in_seq >> 5) & (p.s_row_waves - 1));
+                piece0 = p.s_first + (int64_t)(before + (g * tiles + (in_seq >> tile_shift)) * pieces) * p.s_row_waves + ((in_seq >> 5) & (waves - 1));
             }
             from += 64;
             if (from >= p.num_seqs) break;
-            parts = OwnParts(p, from);
+            parts = Own(p, from);
         }
     }
     auto own_at = [&](int i, int& row) __attribute__((always_inline)) {

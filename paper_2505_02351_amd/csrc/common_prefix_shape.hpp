@@ -49,15 +49,33 @@ struct CommonPlan {
 // Row blocks of a workgroup for so many rows: 1, 2 or 4 of 32.
 inline int common_row_waves(int64_t rows) { return rows > 64 ? 4 : rows > 32 ? 2 : 1; }
 
+// Ranges of the prefix for trees, which bring many rows: `units` KV heads times row tiles, each of `steps` steps.  A CU's workgroups, two at a time, take
+// as long as their steps one after another, so what counts are the most workgroups that a CU gets; every range costs the join
+// a hundredth of a step more for each of its pieces (of 32 rows, 33 KB written and read; a step is 0.67 us), a workgroup some 4 steps to begin and
+// end.  (As many ranges as the CUs hold once, the other calls' rule, leave CUs idle where units are more than a few: 16 trees of 20 - 60 behind
+// 8 192 tokens, 32 / 4 heads, E4M3, 180 units: one range 218 us, four 153.  Equal shares that begin and end anywhere, two to a CU, took 150, and
+// 8 % more of every other call: one workgroup's loop over units kept too much in registers.)
+constexpr int kTreeRounds = 4;                                   // workgroups of a CU at most, where ranges are more than one
+inline int64_t tree_ranges(int64_t units, int64_t steps, int64_t slots, int64_t cus)
+{
+    int64_t best = 1, least = INT64_MAX;
+    for (int64_t n = 1; n == 1 || (units * n <= kTreeRounds * cus && 2 * n <= steps); ++n) {
+        const int64_t cost = 100 * ((units * n + cus - 1) / cus) * ((steps + n - 1) / n + 4) + n * slots;
+        if (cost < least) best = n, least = cost;
+    }
+    return best;
+}
+
 // Shares of all own parts: half a workgroup to a CU beside the prefix's; trees with no prefix have the CUs to themselves, two
-// workgroups to each.
+// workgroups to each.  (1, 2, 3, 4 and 6 to a CU: two trees of 64 behind 32 000, 64 / 8 heads, the first launch alone, 323, 214, 222, 207 and 199 us; with the
+// join 206 at 2, 217 at 3, 212 at 4.  64 trees of 12 - 24 behind 511 - 2 047, 32 / 8, 110, 111 and 114 at 2, 3 and 4.)
 inline int64_t common_most_shares(int64_t cus, bool alone) { return std::max<int64_t>(alone ? 2 * cus : cus / 2, 1); }
 
 // Pieces that any call has that is no larger in its tokens, sequences, prefix, longest context and new tokens of a sequence: what is
 // held for a call serves all smaller ones.  (The pieces of the calls themselves go up and down: a workgroup's worth of rows more
 // means fewer ranges of the prefix.)
 inline int64_t common_held(int64_t rows, int64_t num_seqs, int64_t own_rows, int num_kv_heads, int64_t prefix_len, int64_t max_context_len, int64_t cus,
-                           int64_t most_shares)
+                           int64_t most_shares, bool tree)
 {
     int64_t prefix = 0, own = 0;
     if (prefix_len > 0) {
@@ -65,6 +83,8 @@ inline int64_t common_held(int64_t rows, int64_t num_seqs, int64_t own_rows, int
         // times either is at most 4 cus / KV heads, or s keys / 64.
         const int64_t slots = (rows + 31) / 32;
         prefix = num_kv_heads * std::max(slots, std::min(4 * (cus / num_kv_heads), slots * std::max<int64_t>(prefix_len / 64, 1)));
+        // (tree_ranges: as many times either, and fewer than 2 kTreeRounds cus / KV heads slots of 4 row blocks)
+        if (tree) prefix = num_kv_heads * std::max(slots, std::min(8 * kTreeRounds * (cus / num_kv_heads) + 4, slots * std::max<int64_t>(prefix_len / 64, 1)));
     }
     // (a shorter prefix leaves all of the context behind it)
     for (int w = 1; max_context_len > 0 && w <= common_row_waves(own_rows); w *= 2) {
@@ -93,7 +113,8 @@ inline bool plan_common(CommonPlan& c, int64_t num_tokens, int64_t num_seqs, int
         c.p_tiles = (int)((c.p_slots + c.p_row_waves - 1) / c.p_row_waves);
         // ranges: none shorter than two tiles of 32 for each key group of a workgroup
         const int64_t step = 32 * (kCommonWaves / c.p_row_waves), units = (int64_t)num_kv_heads * c.p_tiles;
-        const int64_t n = std::max<int64_t>(std::min(cus / units, prefix_len / (2 * step)), 1);
+        const int64_t n = tree ? tree_ranges(units, (prefix_len + step - 1) / step, c.p_slots * num_kv_heads, cus)
+                               : std::max<int64_t>(std::min(cus / units, prefix_len / (2 * step)), 1);
         const int64_t each = ((prefix_len + n - 1) / n + step - 1) / step * step;
         c.p_keys = (int)each;
         c.p_splits = (int)((prefix_len + each - 1) / each);
@@ -114,7 +135,7 @@ inline bool plan_common(CommonPlan& c, int64_t num_tokens, int64_t num_seqs, int
         c.s_workgroups = c.s_shares + num_kv_heads * (c.rows / tile_rows + num_seqs);
     }
     if (c.workgroups() > kCommonMostWorkgroups) return false;
-    c.held = common_held(c.rows, num_seqs, own_rows, num_kv_heads, prefix_len, max_context_len, cus, common_most_shares(cus, tree));
+    c.held = common_held(c.rows, num_seqs, own_rows, num_kv_heads, prefix_len, max_context_len, cus, common_most_shares(cus, tree), tree);
     return true;
 }
 

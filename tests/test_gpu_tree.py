@@ -156,6 +156,15 @@ def test_long_contexts_and_many_sequences(G, kv8, B, lens, new, NP):  # noqa: F8
     t.check(t.run(G, bounds=(999, 14)))
 
 
+@pytest.mark.parametrize("kv8", [False, True])
+def test_many_row_tiles_over_a_prefix(G, kv8):  # noqa: F811
+    """More row tiles than fill the CUs once in one range of keys, sequences of one, two and four row blocks to a workgroup."""
+    rng = np.random.RandomState(2)
+    new = [int(n) for n in rng.randint(1, 40, 40)]
+    t = Trees(2, "f16", 32, 16, 64, 16, 20, [320 + n + int(rng.randint(0, 90)) for n in new], new, slopes=True, kv8=kv8).upload()
+    t.check(t.run(G))
+
+
 def test_rows_that_see_nothing(G):  # noqa: F811
     """No context and an empty mask: +0, whatever the neighbours see."""
     t = Trees(3, "f16", 8, 2, 64, 16, 0, [40, 3, 70], [40, 3, 33], kind="any")
