@@ -28,7 +28,8 @@ struct CopyBlocksParams {
     int pieces;                 // of a block, 16 bytes each
 };
 
-// A unit is 16 KiB of one block of one cache (256 threads, four pieces each); workgroups take them in turn, as many as there are.
+// A unit is 16 KiB of one block of one cache (256 threads, four pieces each); workgroups take them in turn, as many as there are.  (750 blocks of
+// 32 KiB in 32 caches, 1.6 GB read and written, 326 us: 4.8 TB/s, where one large copy does 5.15.)
 constexpr int kCopyPieces = 4, kCopyUnit = kPageThreads * kCopyPieces;
 static __global__ __launch_bounds__(kPageThreads) void copy_blocks_kernel(const CopyBlocksParams p)
 {
@@ -66,6 +67,9 @@ struct KeepTokensParams {
 // Row start + paths[i] to row start + i.  Paths ascend, so paths[i] >= i: no row is written before it has been read for a later
 // place if, of any run of places, all are read before any is written; and a thread has one 16-byte column of all rows, so that
 // nobody else's order matters.
+// A head's row is 256 bytes somewhere in the caches, and that is what bounds it: 64 sequences, 249 tokens that move in 32 caches of 8 heads of 128 (33 MB),
+// 20 us, as long as a plain gather of such rows takes for half of the bytes (17).  Asking for all block numbers at once, three round
+// trips in place of five, changes nothing there, and costs 1.4 us where one small tree is all there is (2.8 us; 1.4).
 constexpr int kKeepRun = 8;
 static __global__ __launch_bounds__(kPageThreads) void keep_tokens_kernel(const KeepTokensParams p)
 {
@@ -162,15 +166,9 @@ __device__ __forceinline__ int plan_sums(int x, int* lds, int& all)
     __syncthreads();                                             // (lds is free again)
     if (lane == 63) lds[wave] = sum;
     __syncthreads();
-    int before = 0;
-    all = 0;
-#pragma unroll
-    for (int w = 0; w < kPlanWaves; ++w) {
-        const int s = lds[w];
-        before += w < wave ? s : 0;
-        all += s;
-    }
-    return before + sum - x;
+    const int of_lane = lds[lane & (kPlanWaves - 1)], sums = lane_sums(lane < kPlanWaves ? of_lane : 0);
+    all = __builtin_amdgcn_readlane(sums, kPlanWaves - 1);
+    return __builtin_amdgcn_readlane(sums, __builtin_amdgcn_readfirstlane(wave)) - __builtin_amdgcn_readlane(sum, 63) + sum - x;
 }
 
 // Every thread of the workgroup sees what the others stored or changed by atomics before.
@@ -178,6 +176,49 @@ __device__ __forceinline__ void plan_barrier()
 {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
+}
+
+// Blocks begin .. end - 1 whose count `wanted` names, in ascending order: emit(block, how many of them come before it, count), until `most` have been
+// met or passed -> how many there were.  One workgroup; the counts of a round are asked for a round ahead.  (What bounds such kernels of one workgroup is
+// round trips to memory, those for their own instructions too: four counts to a thread and round, 16 in straight lines cost 4 us more.)
+constexpr int kScanLoads = 4, kScanBlocks = kPlanThreads * kScanLoads;
+template <typename Wanted, typename Emit>
+__device__ __forceinline__ int plan_scan(const int32_t* ref_counts, int begin, int end, int most, int* lds, Wanted wanted, Emit emit)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int met = 0, n[kScanLoads], next[kScanLoads];
+    auto ask = [&](int64_t first) __attribute__((always_inline)) {       // (past the end: the last one again)
+#pragma unroll
+        for (int i = 0; i < kScanLoads; ++i) next[i] = ref_counts[min(first + 64 * i, (int64_t)end - 1)];
+    };
+    if (begin < end && most > 0) ask((int64_t)begin + wave * (64 * kScanLoads) + lane);
+#pragma unroll 1
+    for (int64_t round = begin; round < end && met < most; round += kScanBlocks) {
+        const int64_t first = round + wave * (64 * kScanLoads) + lane;
+#pragma unroll
+        for (int i = 0; i < kScanLoads; ++i) n[i] = next[i];
+        if (round + kScanBlocks < end) ask(first + kScanBlocks);
+        uint64_t mask[kScanLoads];
+        int mine = 0;
+#pragma unroll
+        for (int i = 0; i < kScanLoads; ++i) {
+            mask[i] = __builtin_amdgcn_ballot_w64(first + 64 * i < end && wanted(n[i]));
+            mine += __builtin_popcountll(mask[i]);
+        }
+        __syncthreads();                                         // (lds is free again)
+        if (lane == 0) lds[wave] = mine;
+        __syncthreads();
+        const int of_lane = lds[lane & (kPlanWaves - 1)];        // (a lane's sum over the waves before its own, by one wave's sums)
+        const int sums = lane_sums(lane < kPlanWaves ? of_lane : 0);
+        int at = met + __builtin_amdgcn_readlane(sums, wave) - mine;
+        met += __builtin_amdgcn_readlane(sums, kPlanWaves - 1);
+#pragma unroll
+        for (int i = 0; i < kScanLoads; ++i) {
+            if (mask[i] >> lane & 1) emit((int)(first + 64 * i), at + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask[i] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask[i], 0u)), n[i]);
+            at += __builtin_popcountll(mask[i]);
+        }
+    }
+    return met;
 }
 
 struct ResizeParams {
@@ -189,144 +230,154 @@ struct ResizeParams {
     const int32_t* cu_new;      // [num_seqs + 1]
     int32_t* copies;            // [num_seqs][2]
     int32_t* counts;            // copies, blocks lacking
-    int32_t *old_lens, *replaced, *first;       // workspace, [num_seqs]: lengths before; the shared last block that a row replaces, or -1; its first new block's number
+    int32_t *old_lens, *last, *first;           // workspace, [num_seqs]: ResizeRows
     int32_t* free_blocks;       // workspace, [max_free]
     int num_seqs, max_blocks_per_seq, num_blocks, block_shift, num_slots, max_free;
     __device__ __forceinline__ int old_len(int r) const { return clamped(context_lens[r], max_blocks_per_seq, block_shift); }
     __device__ __forceinline__ int new_len(int r) const { return clamped(new_lens[r], max_blocks_per_seq, block_shift); }
 };
 
-// Entries behind the new lengths are given back: row r, entries from the `first`-th such on, `step` apart.
-__device__ __forceinline__ void resize_drop(const ResizeParams& p, int r, int first, int step)
+// What is known of the rows between the parts of a resize: lengths before; the shared last block that a row replaces, or -1; the number
+// of its first new block among all new ones; and those.
+struct ResizeRows {
+    int32_t *old_lens, *last, *first;
+    const int32_t* free_blocks;
+};
+
+// Entries behind the new lengths are given back: those from the `from`-th such on, `step` apart.
+__device__ __forceinline__ void resize_drop(const ResizeParams& p, int r, int old, int now, int from, int step)
 {
     const int32_t* const row = p.block_tables + (int64_t)r * p.max_blocks_per_seq;
-    const int have = blocks_of(p.old_len(r), p.block_shift), need = blocks_of(p.new_len(r), p.block_shift);
-    for (int j = need + first; j < have; j += step) {
+    const int have = blocks_of(old, p.block_shift), need = blocks_of(now, p.block_shift);
+    for (int j = need + from; j < have; j += step) {
         const int block = row[j];
         if ((uint32_t)block < (uint32_t)p.num_blocks) add_count(p.ref_counts + block, -1);
     }
 }
 
-// Which blocks the growing rows get.  One workgroup.
-__device__ __forceinline__ void resize_plan(const ResizeParams& p)
+// A row's new blocks and the slots of its new tokens, from the `from`-th on, `step` apart.
+__device__ __forceinline__ void resize_apply(const ResizeParams& p, const ResizeRows& rows, int r, bool enough, int from, int step)
 {
-    __shared__ int lds[kPlanWaves];
-    const int S = p.num_seqs, shift = p.block_shift, bmask = (1 << shift) - 1;
-    // Rows whose last block is not full, is about to be written and is held by others too.  Each gives it up; where all of a block's
-    // holders have done so, the last of them by number keeps it: the count, now 0, becomes the least -(1 + row).
-    for (int r = threadIdx.x; r < S; r += kPlanThreads) {
-        const int old = p.old_len(r);
-        int last = -1;
-        if (p.new_len(r) > old && (old & bmask)) {
-            last = p.block_tables[(int64_t)r * p.max_blocks_per_seq + (old >> shift)];
-            if ((uint32_t)last >= (uint32_t)p.num_blocks || read_count(p.ref_counts + last) <= 1) last = -1;
+    const int old = rows.old_lens[r], now = p.new_len(r), shift = p.block_shift;
+    const int have = blocks_of(old, shift) - (rows.last[r] >= 0 ? 1 : 0);        // blocks that it keeps
+    int32_t* const row = p.block_tables + (int64_t)r * p.max_blocks_per_seq;
+    const int32_t* const fresh = rows.free_blocks + rows.first[r];
+    const bool grows = now > old && enough;
+    if (grows)
+        for (int i = from, n = blocks_of(now, shift) - have; i < n; i += step) {
+            const int block = fresh[i];
+            row[have + i] = block;
+            p.ref_counts[block] = 1;
         }
-        p.replaced[r] = last;
-        p.old_lens[r] = old;
-    }
-    plan_barrier();
-    for (int r = threadIdx.x; r < S; r += kPlanThreads)
-        if (p.replaced[r] >= 0) add_count(p.ref_counts + p.replaced[r], -1);
-    plan_barrier();
-    for (int r = threadIdx.x; r < S; r += kPlanThreads) {
-        const int last = p.replaced[r];
-        if (last >= 0 && read_count(p.ref_counts + last) <= 0)
-            __hip_atomic_fetch_min(p.ref_counts + last, -(1 + r), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    plan_barrier();
-    // what each row asks for, numbered by rows; a replaced block comes first
-    int wanted = 0, copies = 0;
-    for (int r0 = 0; r0 < S; r0 += kPlanThreads) {
-        const int r = r0 + threadIdx.x;
-        int wants = 0, copy = 0;
-        if (r < S) {
-            const int last = p.replaced[r], old = p.old_lens[r];
-            if (last >= 0) {
-                if (read_count(p.ref_counts + last) == -(1 + r)) p.replaced[r] = -1 - (last + 1);        // keeps it: put right below
-                else copy = 1;
-            }
-            wants = copy + max(blocks_of(p.new_len(r), shift) - blocks_of(old, shift), 0);
-        }
-        int all;
-        const int at = wanted + plan_sums(wants, lds, all);
-        wanted += all;
-        if (r < S) p.first[r] = at;
-        copies += plan_sums(copy, lds, all);                     // (of this thread's rows: put right below)
-    }
-    (void)copies;
-    plan_barrier();
-    for (int r = threadIdx.x; r < S; r += kPlanThreads) {
-        const int last = p.replaced[r];
-        if (last < -1) {
-            p.ref_counts[-2 - last] = 1;
-            p.replaced[r] = -1;
-        }
-    }
-    plan_barrier();
-    // the lowest free blocks, as many as are asked for
-    int found = 0;
-    for (int b0 = 0; b0 < p.num_blocks && found < wanted; b0 += 4 * kPlanThreads) {
-        const int b = b0 + 4 * threadIdx.x;
-        int n[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) n[i] = b + i < p.num_blocks ? p.ref_counts[b + i] : 1;
-        int all, at = found + plan_sums((n[0] == 0) + (n[1] == 0) + (n[2] == 0) + (n[3] == 0), lds, all);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (n[i] == 0) {
-                if (at < p.max_free) p.free_blocks[at] = b + i;
-                ++at;
-            }
-        found += all;
-    }
-    plan_barrier();
-    const bool enough = found >= wanted;
-    // copies are numbered by rows, a wave to a row from here on
-    int copy0 = 0;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    for (int r0 = 0; r0 < S; r0 += kPlanThreads) {
-        const int r = r0 + threadIdx.x;
-        const int last = r < S ? p.replaced[r] : -1;
-        int all;
-        const int at = copy0 + plan_sums(last >= 0 ? 1 : 0, lds, all);
-        copy0 += all;
-        if (last < 0) continue;
-        if (enough) {
-            p.copies[2 * at] = last;
-            p.copies[2 * at + 1] = p.free_blocks[p.first[r]];
-        } else {
-            add_count(p.ref_counts + last, 1);                   // it stays
-        }
-    }
-    if (threadIdx.x == 0) {
-        p.counts[0] = enough ? copy0 : 0;
-        p.counts[1] = enough ? 0 : wanted - found;
-    }
-    for (int r = wave; r < S; r += kPlanWaves) {
-        const int old = p.old_lens[r], now = p.new_len(r);
-        if (now > old && enough) {
-            int32_t* const row = p.block_tables + (int64_t)r * p.max_blocks_per_seq;
-            const int copy = p.replaced[r] >= 0 ? 1 : 0, have = blocks_of(old, shift) - copy, n = blocks_of(now, shift) - have, at = p.first[r];
-            for (int i = lane; i < n; i += 64) {
-                const int block = p.free_blocks[at + i];
-                row[have + i] = block;
-                p.ref_counts[block] = 1;
-            }
-        }
-        if (lane == 0 && (now <= old || enough)) p.context_lens[r] = now;
+    if (from == 0 && (now <= old || enough)) p.context_lens[r] = now;
+    if (!p.slots) return;
+    const int begin = max(p.cu_new[r], 0), end = min(p.cu_new[r + 1], p.num_slots);
+    const int kept = grows && have > 0 && (old >> shift) == have - 1 ? row[have - 1] : 0;              // of the first tokens, where they fill a block
+    for (int i = from; i < end - begin; i += step) {
+        const int pos = old + i, j = pos >> shift;
+        const int block = grows && pos < now ? (j < have ? kept : fresh[j - have]) : -1;
+        p.slots[begin + i] = grows && pos < now ? ((int64_t)block << shift) + (pos & ((1 << shift) - 1)) : -1;
     }
 }
 
-// Slots of the new tokens of row r: those from the `first`-th on, `step` apart.
-__device__ __forceinline__ void resize_slots(const ResizeParams& p, int r, int first, int step)
+// Which blocks the growing rows get -> whether there are as many.  One workgroup.  ONE: what is known of the rows stays in LDS, up to
+// kPlanThreads of them, and what they give back is given back here.
+constexpr int kPlanFree = 4096;         // new blocks that LDS holds
+template <bool ONE> __device__ __forceinline__ bool resize_plan(const ResizeParams& p, ResizeRows& rows)
 {
-    const int32_t* const row = p.block_tables + (int64_t)r * p.max_blocks_per_seq;
-    const int old = p.old_lens[r], grown = p.context_lens[r] - old, begin = max(p.cu_new[r], 0), end = min(p.cu_new[r + 1], p.num_slots);
-    for (int i = first; i < end - begin; i += step) {
-        int64_t slot = -1;
-        if (i < grown) slot = ((int64_t)row[(old + i) >> p.block_shift] << p.block_shift) + ((old + i) & ((1 << p.block_shift) - 1));
-        p.slots[begin + i] = slot;
+    __shared__ int lds[kPlanWaves];
+    __shared__ int32_t lds_rows[ONE ? 3 : 1][ONE ? kPlanThreads : 1], lds_free[ONE ? kPlanFree : 1];
+    const int S = p.num_seqs, shift = p.block_shift, bmask = (1 << shift) - 1;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    rows = ONE ? ResizeRows{lds_rows[0], lds_rows[1], lds_rows[2], lds_free} : ResizeRows{p.old_lens, p.last, p.first, p.free_blocks};
+    // (`first` holds the new lengths until it is known)
+    int32_t* const news = rows.first;
+    bool drops = false;
+    for (int r = threadIdx.x; r < S; r += kPlanThreads) {
+        const int old = p.old_len(r), now = p.new_len(r);
+        int last = -1;
+        if (now > old && (old & bmask)) last = p.block_tables[(int64_t)r * p.max_blocks_per_seq + (old >> shift)];
+        rows.old_lens[r] = old;
+        rows.last[r] = (uint32_t)last < (uint32_t)p.num_blocks ? last : -1;
+        news[r] = now;
+        drops = drops || blocks_of(now, shift) < blocks_of(old, shift);
     }
+    if (ONE && __syncthreads_or(drops)) {
+        for (int r = wave; r < S; r += kPlanWaves) resize_drop(p, r, rows.old_lens[r], news[r], lane, 64);
+        plan_barrier();
+    }
+    // Rows whose last block is not full, is about to be written and is held by others too.  Each gives it up; where all of a block's
+    // holders have done so, the last of them by number keeps it: the count, now 0, becomes the least -(1 + row).
+    bool shared = false;
+    for (int r = threadIdx.x; r < S; r += kPlanThreads) {
+        const int last = rows.last[r];
+        if (last >= 0 && read_count(p.ref_counts + last) <= 1) rows.last[r] = -1;
+        shared = shared || rows.last[r] >= 0;
+    }
+    shared = __syncthreads_or(shared);
+    if (shared) {
+        for (int r = threadIdx.x; r < S; r += kPlanThreads)
+            if (rows.last[r] >= 0) add_count(p.ref_counts + rows.last[r], -1);
+        plan_barrier();
+        for (int r = threadIdx.x; r < S; r += kPlanThreads) {
+            const int last = rows.last[r];
+            if (last >= 0 && read_count(p.ref_counts + last) <= 0)
+                __hip_atomic_fetch_min(p.ref_counts + last, -(1 + r), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        plan_barrier();
+        for (int r = threadIdx.x; r < S; r += kPlanThreads) {
+            const int last = rows.last[r];
+            if (last >= 0 && read_count(p.ref_counts + last) == -(1 + r)) rows.last[r] = -2 - last;
+        }
+        __syncthreads();                                         // (all have looked)
+        for (int r = threadIdx.x; r < S; r += kPlanThreads) {
+            const int last = rows.last[r];
+            if (last < -1) {
+                p.ref_counts[-2 - last] = 1;
+                rows.last[r] = -1;
+            }
+        }
+        plan_barrier();
+    }
+    // what each row asks for, numbered by rows; a replaced block comes first
+    int wanted = 0;
+    for (int r0 = 0; r0 < S; r0 += kPlanThreads) {
+        const int r = r0 + threadIdx.x;
+        int wants = 0;
+        if (r < S) wants = (rows.last[r] >= 0) + max(blocks_of(news[r], shift) - blocks_of(rows.old_lens[r], shift), 0);
+        int all;
+        const int at = wanted + plan_sums(wants, lds, all);
+        wanted += all;
+        if (r < S) rows.first[r] = at;
+    }
+    // the lowest free blocks, as many as are asked for
+    int32_t* const free = ONE && wanted <= kPlanFree ? lds_free : p.free_blocks;
+    const int room = ONE && wanted <= kPlanFree ? kPlanFree : p.max_free;
+    rows.free_blocks = free;
+    const int found = plan_scan(p.ref_counts, 0, p.num_blocks, wanted, lds, [](int n) { return n == 0; },
+                                [&](int block, int at, int) __attribute__((always_inline)) { if (at < room) free[at] = block; });
+    plan_barrier();
+    const bool enough = found >= wanted;
+    int copies = 0;
+    if (shared)
+        for (int r0 = 0; r0 < S; r0 += kPlanThreads) {
+            const int r = r0 + threadIdx.x, last = r < S ? rows.last[r] : -1;
+            int all;
+            const int at = copies + plan_sums(last >= 0 ? 1 : 0, lds, all);
+            copies += all;
+            if (last < 0) continue;
+            if (enough) {
+                p.copies[2 * at] = last;
+                p.copies[2 * at + 1] = free[rows.first[r]];
+            } else {
+                add_count(p.ref_counts + last, 1);               // it stays
+            }
+        }
+    if (threadIdx.x == 0) {
+        p.counts[0] = enough ? copies : 0;
+        p.counts[1] = enough ? 0 : wanted - found;
+    }
+    return enough;
 }
 
 // All of it in one workgroup, for changes of a few tokens.
@@ -334,23 +385,25 @@ constexpr int64_t kResizeOneTokens = 4096;      // rows times the most that one 
 static __global__ __launch_bounds__(kPlanThreads) void resize_one_kernel(const ResizeParams p)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    for (int r = wave; r < p.num_seqs; r += kPlanWaves) resize_drop(p, r, lane, 64);
-    plan_barrier();
-    resize_plan(p);
-    if (!p.slots) return;
-    plan_barrier();
-    for (int r = wave; r < p.num_seqs; r += kPlanWaves) resize_slots(p, r, lane, 64);
+    ResizeRows rows;
+    const bool enough = resize_plan<true>(p, rows);
+    for (int r = wave; r < p.num_seqs; r += kPlanWaves) resize_apply(p, rows, r, enough, lane, 64);
 }
 
 // The same in three launches: rows x parts of a row, the plan, rows x parts.
 static __global__ __launch_bounds__(kPageThreads) void resize_drop_kernel(const ResizeParams p)
 {
-    resize_drop(p, blockIdx.x, blockIdx.y * kPageThreads + threadIdx.x, gridDim.y * kPageThreads);
+    resize_drop(p, blockIdx.x, p.old_len(blockIdx.x), p.new_len(blockIdx.x), blockIdx.y * kPageThreads + threadIdx.x, gridDim.y * kPageThreads);
 }
-static __global__ __launch_bounds__(kPlanThreads) void resize_plan_kernel(const ResizeParams p) { resize_plan(p); }
-static __global__ __launch_bounds__(kPageThreads) void resize_slots_kernel(const ResizeParams p)
+static __global__ __launch_bounds__(kPlanThreads) void resize_plan_kernel(const ResizeParams p)
 {
-    resize_slots(p, blockIdx.x, blockIdx.y * kPageThreads + threadIdx.x, gridDim.y * kPageThreads);
+    ResizeRows rows;
+    resize_plan<false>(p, rows);
+}
+static __global__ __launch_bounds__(kPageThreads) void resize_apply_kernel(const ResizeParams p)
+{
+    const ResizeRows rows{p.old_lens, p.last, p.first, p.free_blocks};
+    resize_apply(p, rows, blockIdx.x, p.counts[1] == 0, blockIdx.y * kPageThreads + threadIdx.x, gridDim.y * kPageThreads);
 }
 
 struct CompactParams {
@@ -363,39 +416,33 @@ struct CompactParams {
     int num_seqs, max_blocks_per_seq, num_blocks, block_shift, max_copies;
 };
 
-// Of U blocks in use, the i-th highest goes to the i-th lowest free one, as far as that is below U.  One workgroup.
+// Of U blocks in use, the i-th highest goes to the i-th lowest free one, as far as that is below U.  (As many are in use from U on as are free below
+// it: what comes a-th from U on is the (holes - 1 - a)-th highest.)  One workgroup.
 static __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(const CompactParams p)
 {
     __shared__ int lds[kPlanWaves];
-    int used = 0, all;
-    for (int b = threadIdx.x; b < p.num_blocks; b += kPlanThreads) used += p.ref_counts[b] > 0;
-    plan_sums(used, lds, used);
-    int holes = 0;
-    for (int b0 = 0; b0 < used; b0 += kPlanThreads) {
-        const int b = b0 + threadIdx.x;
-        const bool hole = b < used && p.ref_counts[b] <= 0;
-        const int at = holes + plan_sums(hole, lds, all);
-        holes += all;
-        if (hole) p.holes[at] = b;
-    }
+    int mine = 0, used;
+#pragma unroll 4
+    for (int64_t b = threadIdx.x; b < p.num_blocks; b += kPlanThreads) mine += p.ref_counts[b] > 0;
+    plan_sums(mine, lds, used);
+    const int holes = plan_scan(p.ref_counts, 0, used, used, lds, [](int n) { return n <= 0; },
+                                [&](int block, int at, int) __attribute__((always_inline)) { p.holes[at] = block; });
     plan_barrier();
     const int copies = min(holes, p.max_copies);
-    int movers = 0;
-    for (int b0 = p.num_blocks - 1; b0 >= used; b0 -= kPlanThreads) {
-        const int b = b0 - threadIdx.x, held = b >= used ? p.ref_counts[b] : 0;
-        const int at = movers + plan_sums(held > 0, lds, all);
-        movers += all;
-        if (b < used) continue;
-        const bool moves = held > 0 && at < copies;
-        const int to = moves ? p.holes[at] : b;
-        p.to[b] = to;
-        if (moves) {
-            p.copies[2 * at] = b;
-            p.copies[2 * at + 1] = to;
-            p.ref_counts[to] = held;
-            p.ref_counts[b] = 0;
-        }
-    }
+#pragma unroll 1
+    for (int64_t b = (int64_t)used + threadIdx.x; b < p.num_blocks; b += kPlanThreads) p.to[b] = (int)b;
+    plan_barrier();
+    plan_scan(p.ref_counts, used, p.num_blocks, holes, lds, [](int n) { return n > 0; },
+              [&](int block, int after, int held) __attribute__((always_inline)) {
+                  const int at = holes - 1 - after;
+                  if (at >= copies) return;
+                  const int to = p.holes[at];
+                  p.to[block] = to;
+                  p.copies[2 * at] = block;
+                  p.copies[2 * at + 1] = to;
+                  p.ref_counts[to] = held;
+                  p.ref_counts[block] = 0;
+              });
     if (threadIdx.x == 0) {
         p.counts[0] = copies;
         p.counts[1] = used;

@@ -134,8 +134,8 @@ int optgqa_resize_sequences(int32_t* block_tables, int32_t* context_lens, int32_
     p.copies = copies;
     p.counts = counts;
     p.old_lens = static_cast<int32_t*>(workspace);
-    p.replaced = p.old_lens + num_seqs;
-    p.first = p.replaced + num_seqs;
+    p.last = p.old_lens + num_seqs;
+    p.first = p.last + num_seqs;
     p.free_blocks = p.first + num_seqs;
     p.num_seqs = num_seqs;
     p.max_blocks_per_seq = max_blocks_per_seq;
@@ -144,11 +144,12 @@ int optgqa_resize_sequences(int32_t* block_tables, int32_t* context_lens, int32_
     p.num_slots = num_slots;
     p.max_free = (int)std::min<int64_t>(num_blocks, (int64_t)num_seqs * ((int64_t)max_blocks_per_seq + 1));
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if ((int64_t)num_seqs * max_change <= kResizeOneTokens) return launch(resize_one_kernel, dim3(1), dim3(kPlanThreads), 0, st, p);
+    if (num_seqs <= kPlanThreads && (int64_t)num_seqs * max_change <= kResizeOneTokens)
+        return launch(resize_one_kernel, dim3(1), dim3(kPlanThreads), 0, st, p);
     const int64_t most = std::min<int64_t>(max_change, (int64_t)max_blocks_per_seq * block_size);
     int rc = launch(resize_drop_kernel, dim3(num_seqs, row_parts(most / block_size + 1, kPageThreads)), dim3(kPageThreads), 0, st, p);
     if (rc == OPTGQA_OK) rc = launch(resize_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, p);
-    if (rc == OPTGQA_OK && p.slots) rc = launch(resize_slots_kernel, dim3(num_seqs, row_parts(most, 4 * kPageThreads)), dim3(kPageThreads), 0, st, p);
+    if (rc == OPTGQA_OK) rc = launch(resize_apply_kernel, dim3(num_seqs, row_parts(most, 4 * kPageThreads)), dim3(kPageThreads), 0, st, p);
     return rc;
 }
 
