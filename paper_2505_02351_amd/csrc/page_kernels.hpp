@@ -20,6 +20,13 @@ __device__ __forceinline__ int blocks_of(int tokens, int shift) { return (int)((
 
 // ---- rows of caches ---------------------------------------------------------------------------------------------
 
+__device__ __forceinline__ void stream_store16(void* p, uint4 x)
+{
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    const u32x4 v = {x.x, x.y, x.z, x.w};
+    __builtin_nontemporal_store(v, static_cast<u32x4*>(p));
+}
+
 struct CopyBlocksParams {
     unsigned char* const* caches;
     const int32_t* copies;      // [max_copies][2]: from, to
@@ -28,8 +35,9 @@ struct CopyBlocksParams {
     int pieces;                 // of a block, 16 bytes each
 };
 
-// A unit is 16 KiB of one block of one cache (256 threads, four pieces each); workgroups take them in turn, as many as there are.  (750 blocks of
-// 32 KiB in 32 caches, 1.6 GB read and written, 326 us: 4.8 TB/s, where one large copy does 5.15.)
+// A unit is 16 KiB of one block of one cache (256 threads, four pieces each); workgroups take them in turn, eight to a CU.  Memory bounds it: 750 blocks of
+// 32 KiB in 32 caches, 1.57 GB read and written, 311 us, 5.05 TB/s, where one large copy does 5.15.  (The whole pass 322 us; 336 through the caches, 318 with
+// a workgroup to each unit, which costs the usual call, whose bound is far above what there is to copy; 8 KiB units 385, 32 KiB 511.)
 constexpr int kCopyPieces = 4, kCopyUnit = kPageThreads * kCopyPieces;
 static __global__ __launch_bounds__(kPageThreads) void copy_blocks_kernel(const CopyBlocksParams p)
 {
@@ -47,10 +55,10 @@ static __global__ __launch_bounds__(kPageThreads) void copy_blocks_kernel(const 
         uint4 x[kCopyPieces];
 #pragma unroll
         for (int i = 0; i < kCopyPieces; ++i)
-            if (first + i * kPageThreads < p.pieces) x[i] = src[first + i * kPageThreads];
+            if (first + i * kPageThreads < p.pieces) x[i] = stream_load16(src + first + i * kPageThreads);
 #pragma unroll
         for (int i = 0; i < kCopyPieces; ++i)
-            if (first + i * kPageThreads < p.pieces) dst[first + i * kPageThreads] = x[i];
+            if (first + i * kPageThreads < p.pieces) stream_store16(dst + first + i * kPageThreads, x[i]);
     }
 }
 
@@ -414,7 +422,19 @@ struct CompactParams {
     int32_t* counts;            // copies, blocks in use
     int32_t *holes, *to;        // workspace, [num_blocks] each: free blocks below the number in use; where a block from there on goes
     int num_seqs, max_blocks_per_seq, num_blocks, block_shift, max_copies;
+    bool tables_too;            // few entries: the plan's workgroup changes them as well
 };
+
+// Entries of row r, from the `from`-th on, `step` apart.
+__device__ __forceinline__ void compact_row(const CompactParams& p, int used, int r, int from, int step)
+{
+    const int n = blocks_of(clamped(p.context_lens[r], p.max_blocks_per_seq, p.block_shift), p.block_shift);
+    int32_t* const row = p.block_tables + (int64_t)r * p.max_blocks_per_seq;
+    for (int j = from; j < n; j += step) {
+        const int block = row[j];
+        if (block >= used && block < p.num_blocks) row[j] = p.to[block];
+    }
+}
 
 // Of U blocks in use, the i-th highest goes to the i-th lowest free one, as far as that is below U.  (As many are in use from U on as are free below
 // it: what comes a-th from U on is the (holes - 1 - a)-th highest.)  One workgroup.
@@ -447,16 +467,14 @@ static __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(const
         p.counts[0] = copies;
         p.counts[1] = used;
     }
+    if (!p.tables_too) return;
+    plan_barrier();
+    for (int r = threadIdx.x >> 6; r < p.num_seqs; r += kPlanWaves) compact_row(p, used, r, threadIdx.x & 63, 64);
 }
 
 static __global__ __launch_bounds__(kPageThreads) void compact_tables_kernel(const CompactParams p)
 {
-    const int used = p.counts[1], n = blocks_of(clamped(p.context_lens[blockIdx.x], p.max_blocks_per_seq, p.block_shift), p.block_shift);
-    int32_t* const row = p.block_tables + (int64_t)blockIdx.x * p.max_blocks_per_seq;
-    for (int j = blockIdx.y * kPageThreads + threadIdx.x; j < n; j += gridDim.y * kPageThreads) {
-        const int block = row[j];
-        if (block >= used && block < p.num_blocks) row[j] = p.to[block];
-    }
+    compact_row(p, p.counts[1], blockIdx.x, blockIdx.y * kPageThreads + threadIdx.x, gridDim.y * kPageThreads);
 }
 
 }  // namespace optgqa
