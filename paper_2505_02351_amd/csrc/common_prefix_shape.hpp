@@ -83,8 +83,8 @@ inline int64_t common_held(int64_t rows, int64_t num_seqs, int64_t own_rows, int
         // times either is at most 4 cus / KV heads, or s keys / 64.
         const int64_t slots = (rows + 31) / 32;
         prefix = num_kv_heads * std::max(slots, std::min(4 * (cus / num_kv_heads), slots * std::max<int64_t>(prefix_len / 64, 1)));
-        // (tree_ranges: as many times either, and fewer than 2 kTreeRounds cus / KV heads slots of 4 row blocks)
-        if (tree) prefix = num_kv_heads * std::max(slots, std::min(8 * kTreeRounds * (cus / num_kv_heads) + 4, slots * std::max<int64_t>(prefix_len / 64, 1)));
+        // (tree_ranges: a range for 64 keys begun at most, and kTreeRounds cus workgroups of up to 4 row blocks where they are more than one)
+        if (tree) prefix = num_kv_heads * std::max(slots, std::min(4 * kTreeRounds * cus / num_kv_heads + 1, slots * ((prefix_len + 63) / 64)));
     }
     // (a shorter prefix leaves all of the context behind it)
     for (int w = 1; max_context_len > 0 && w <= common_row_waves(own_rows); w *= 2) {
