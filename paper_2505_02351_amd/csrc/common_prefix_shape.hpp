@@ -58,6 +58,7 @@ inline int common_row_waves(int64_t rows) { return rows > 64 ? 4 : rows > 32 ? 2
 constexpr int kTreeRounds = 4;                                   // workgroups of a CU at most, where ranges are more than one
 inline int64_t tree_ranges(int64_t units, int64_t steps, int64_t slots, int64_t cus)
 {
+    if (8 * units <= cus) return std::max<int64_t>(std::min(cus / units, steps / 2), 1);          // (they leave an eighth of the CUs idle at most)
     int64_t best = 1, least = INT64_MAX;
     for (int64_t n = 1; n == 1 || (units * n <= kTreeRounds * cus && 2 * n <= steps); ++n) {
         const int64_t cost = 100 * ((units * n + cus - 1) / cus) * ((steps + n - 1) / n + 4) + n * slots;
@@ -67,7 +68,7 @@ inline int64_t tree_ranges(int64_t units, int64_t steps, int64_t slots, int64_t 
 }
 
 // Shares of all own parts: half a workgroup to a CU beside the prefix's; trees with no prefix have the CUs to themselves, two
-// workgroups to each.  (1, 2, 3, 4 and 6 to a CU: two trees of 64 behind 32 000, 64 / 8 heads, the first launch alone, 323, 214, 222, 207 and 199 us; with the
+// workgroups to each, and with one as much of that as their steps are of all.  (1, 2, 3, 4 and 6 to a CU: two trees of 64 behind 32 000, 64 / 8 heads, the first launch alone, 323, 214, 222, 207 and 199 us; with the
 // join 206 at 2, 217 at 3, 212 at 4.  64 trees of 12 - 24 behind 511 - 2 047, 32 / 8, 110, 111 and 114 at 2, 3 and 4.)
 inline int64_t common_most_shares(int64_t cus, bool alone) { return std::max<int64_t>(alone ? 2 * cus : cus / 2, 1); }
 
@@ -130,7 +131,10 @@ inline bool plan_common(CommonPlan& c, int64_t num_tokens, int64_t num_seqs, int
         if (each > (1 << 20) || num_kv_heads * tiles >= (1ll << 30) || num_kv_heads * tiles * each >= (1ll << 30)) return false;
         // (a piece of half of all CUs' share: with more pieces, and with fewer, 64 sequences behind 4 096 tokens, own parts of 127 - 1 023, take
         // 37 - 38 us instead of 32, behind 32 768, 1 023 - 2 047, 110 - 125 instead of 110)
-        c.s_shares = (int)std::min<int64_t>(common_most_shares(cus, tree && prefix_len == 0), num_kv_heads * tiles * each);
+        const int64_t own = num_kv_heads * tiles * each, prefix = c.p_units * c.p_tiles * ((c.p_keys + step - 1) / step);      // steps
+        int64_t most = common_most_shares(cus, false);
+        if (tree) most = std::max<int64_t>(most, (int64_t)(common_most_shares(cus, true) * ((double)own / (double)(own + prefix))));
+        c.s_shares = (int)std::min(most, own);
         // no more than the shares and one for each segment
         c.s_workgroups = c.s_shares + num_kv_heads * (c.rows / tile_rows + num_seqs);
     }
