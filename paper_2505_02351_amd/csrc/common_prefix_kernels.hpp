@@ -743,8 +743,8 @@ __global__ __launch_bounds__(kCommonThreads, 2) void common_prefix_kernel(const 
     else common_body<DT, KV8, D, TREE, 1>(p, job);
 }
 
-// N pieces of a lane's row: i0, i0 + 4, ..; of 8 J of their dims the lane's halves.
-template <int D, int J, int N> struct JoinBatch {
+// N pieces of a lane's row: i0, i0 + STRIDE, ..; of 8 J of their dims the lane's halves.
+template <int D, int J, int N, int STRIDE = kCommonWaves> struct JoinBatch {
     static constexpr int kPieceVectors = D / 8 * 64;
     float2 ml[N];
     float4 x[N][J];
@@ -754,7 +754,7 @@ template <int D, int J, int N> struct JoinBatch {
     {
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            const int i = i0 + kCommonWaves * k;
+            const int i = i0 + STRIDE * k;
             ml[k] = make_float2(-INFINITY, 0.f);
 #pragma unroll
             for (int j = 0; j < J; ++j) x[k][j] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -772,7 +772,7 @@ template <int D, int J, int N> struct JoinBatch {
 template <int J> struct JoinState {
     float m = -INFINITY, l = 0.f;
     float4 acc[J] = {};
-    template <int D, int N> __device__ __forceinline__ void add(const JoinBatch<D, J, N>& b)
+    template <int D, int N, int STRIDE> __device__ __forceinline__ void add(const JoinBatch<D, J, N, STRIDE>& b)
     {
         float m_new = m;
 #pragma unroll
@@ -791,6 +791,37 @@ template <int J> struct JoinState {
                 acc[j].x = fmaf(f, b.x[k][j].x, acc[j].x), acc[j].y = fmaf(f, b.x[k][j].y, acc[j].y);
                 acc[j].z = fmaf(f, b.x[k][j].z, acc[j].z), acc[j].w = fmaf(f, b.x[k][j].w, acc[j].w);
             }
+        }
+    }
+};
+// A row's pieces of its sequence's own part: the steps in which it sees a key, and the workgroups that had them.
+template <bool TREE> struct OwnPieces {
+    int count = 0, row_off = 0;         // how many; how far its row in them lies from row n32
+    int64_t first = 0;
+    __device__ __forceinline__ OwnPieces(const CommonParams& p, const PlaceGuess& guess, OwnParts<TREE>& parts, int t, int g, int rc, int n32)
+    {
+        typedef OwnParts<TREE> Own;
+        if (p.s_shares <= 0) return;
+        const TokenPlace at = guess.find(p, t);
+        const int behind = (TREE ? at.len : at.pos(t) + 1) - p.prefix_len;        // (no sequence: 0)
+        const int share = own_share(p, parts);
+        int all = 0;
+        for (int from = 0;;) {
+            parts.number(share, all);
+            const int l = at.seq - from;                         // (all lanes exchange)
+            const int before = __shfl(parts.before, l & 63), pieces = __shfl(parts.pieces, l & 63), steps = __shfl(parts.steps, l & 63);
+            if (behind > 0 && l >= 0 && l < 64) {
+                const int waves = Own::row_waves_of(p, (at.end - at.first) * p.group);
+                const int in_seq = rc - at.first * p.group, tile_rows = 32 * waves, tile_shift = 31 - __builtin_clz(tile_rows);
+                const int tiles = ((at.end - at.first) * p.group + tile_rows - 1) >> tile_shift;
+                const int each = Own::each(steps, pieces);
+                count = div_by_inverse(Own::steps_of(waves, behind) + each - 1, each, __builtin_amdgcn_rcpf((float)each));
+                row_off = (in_seq & 31) - n32;
+                first = p.s_first + (int64_t)(before + (g * tiles + (in_seq >> tile_shift)) * pieces) * p.s_row_waves + ((in_seq >> 5) & (waves - 1));
+            }
+            from += 64;
+            if (from >= p.num_seqs) break;
+            parts = Own(p, from);
         }
     }
 };
@@ -818,35 +849,11 @@ __global__ __launch_bounds__(kCommonThreads) void common_join_kernel(const Commo
         return ((int64_t)i * p.num_kv_heads + g) * p.p_slots + tile;
     };
     prefix.load(p, o, n32, wave, p.p_splits, prefix_at);
-    // its own: the steps in which it sees a key, and the workgroups that had them
-    int n = 0, row_off = 0;
-    int64_t piece0 = 0;
-    if (p.s_shares > 0) {
-        const TokenPlace at = guess.find(p, t);
-        const int behind = (TREE ? at.len : at.pos(t) + 1) - p.prefix_len;        // (no sequence: 0)
-        const int share = own_share(p, parts);
-        int all = 0;
-        for (int from = 0;;) {
-            parts.number(share, all);
-            const int l = at.seq - from;                         // (all lanes exchange)
-            const int before = __shfl(parts.before, l & 63), pieces = __shfl(parts.pieces, l & 63), steps = __shfl(parts.steps, l & 63);
-            if (behind > 0 && l >= 0 && l < 64) {
-                const int waves = Own::row_waves_of(p, (at.end - at.first) * p.group);
-                const int in_seq = rc - at.first * p.group, tile_rows = 32 * waves, tile_shift = 31 - __builtin_clz(tile_rows);
-                const int tiles = ((at.end - at.first) * p.group + tile_rows - 1) >> tile_shift;
-                const int each = Own::each(steps, pieces);
-                n = div_by_inverse(Own::steps_of(waves, behind) + each - 1, each, __builtin_amdgcn_rcpf((float)each));
-                row_off = (in_seq & 31) - n32;
-                piece0 = p.s_first + (int64_t)(before + (g * tiles + (in_seq >> tile_shift)) * pieces) * p.s_row_waves + ((in_seq >> 5) & (waves - 1));
-            }
-            from += 64;
-            if (from >= p.num_seqs) break;
-            parts = Own(p, from);
-        }
-    }
+    const OwnPieces<TREE> mine(p, guess, parts, t, g, rc, n32);
+    const int n = mine.count;
     auto own_at = [&](int i, int& row) __attribute__((always_inline)) {
-        row = row_off;
-        return piece0 + (int64_t)i * p.s_row_waves;
+        row = mine.row_off;
+        return mine.first + (int64_t)i * p.s_row_waves;
     };
     JoinBatch<D, J, 2> own;
     own.load(p, o, n32, wave, n, own_at);
@@ -887,6 +894,53 @@ __global__ __launch_bounds__(kCommonThreads) void common_join_kernel(const Commo
     packed.x = l_all == 0.f ? 0u : narrow2<DT>(s.x * inv, s.y * inv);
     packed.y = l_all == 0.f ? 0u : narrow2<DT>(s.z * inv, s.w * inv);
     *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + ((int64_t)t * p.num_heads + head) * D + part * DIMS + 8 * wave + 4 * h2) = packed;
+}
+
+// The same for trees whose rows have few pieces: a workgroup has all dims of its 32 rows, a wave a quarter of them and all pieces, so
+// that nothing passes through LDS and no wave goes without a piece.
+template <int DT, int D>
+__global__ __launch_bounds__(kCommonThreads) void tree_join_kernel(const CommonParams p)
+{
+    constexpr int J = D / 32;
+    const int lane = threadIdx.x & 63, n32 = lane & 31, h2 = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tile = p.by_kv_heads.div(blockIdx.x), g = blockIdx.x - tile * p.num_kv_heads;
+    const int r = 32 * tile + n32, rc = min(r, p.rows - 1), t = p.by_group.div(rc), head = g * p.group + (rc - t * p.group);
+    const PlaceGuess guess(p, t);
+    OwnParts<true> parts(p, 0);
+    JoinState<J> state;
+    const float4* const o = p.o + wave * J * 64 + n32 + 32 * h2;
+    auto prefix_at = [&](int i, int& row) __attribute__((always_inline)) {
+        row = 0;
+        return ((int64_t)i * p.num_kv_heads + g) * p.p_slots + tile;
+    };
+    for (int i0 = 0; i0 < p.p_splits; i0 += 4) {
+        JoinBatch<D, J, 4, 1> prefix;
+        prefix.load(p, o, n32, i0, p.p_splits, prefix_at);
+        state.add(prefix);
+    }
+    const OwnPieces<true> mine(p, guess, parts, t, g, rc, n32);
+    auto own_at = [&](int i, int& row) __attribute__((always_inline)) {
+        row = mine.row_off;
+        return mine.first + (int64_t)i * p.s_row_waves;
+    };
+    for (int i0 = 0, most = wave_max(mine.count); i0 < most; i0 += 4) {
+        JoinBatch<D, J, 4, 1> own;
+        own.load(p, o, n32, i0, mine.count, own_at);
+        state.add(own);
+    }
+    if (r >= p.rows) return;
+    // (a row that sees no key: +0; a sum that is no number stays one)
+    const float inv = state.l == 0.f ? 0.f : (p.v_scales ? p.v_scales[g] : p.out_scale) / state.l;
+    uint16_t* const to = static_cast<uint16_t*>(p.out) + ((int64_t)t * p.num_heads + head) * D + wave * (8 * J) + 4 * h2;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        const float4 x = state.acc[j];
+        uint2 packed;
+        packed.x = state.l == 0.f ? 0u : narrow2<DT>(x.x * inv, x.y * inv);
+        packed.y = state.l == 0.f ? 0u : narrow2<DT>(x.z * inv, x.w * inv);
+        *reinterpret_cast<uint2*>(to + 8 * j) = packed;
+    }
 }
 
 }  // namespace optgqa

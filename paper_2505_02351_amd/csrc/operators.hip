@@ -184,6 +184,12 @@ int launch_common(const CommonParams& p, int workgroups, hipStream_t st)
     // 32 dims to a workgroup of the join, 16 where those would not be one to a CU (16 sequences of 32 / 8 heads of 128 behind 6 528
     // tokens: 16.0 us against 16.4; 32 of 3 - 6 new tokens each, 40 / 8 heads: 47.1 against 44.9)
     const int tiles = p.p_slots * p.num_kv_heads;
+    if constexpr (TREE) {
+        // all dims to a workgroup where those are three to four CUs or more: the rows have few pieces then (replayed graphs, us, so many of 32 rows, without and with: 64 trees
+        // of 12 - 24 behind 511 - 2 047 1 160, 111 and 101; 64 of 8 - 24 behind 4 096 1 024, 144 and 132; two of 64 behind 32 000 256, 204 and 204; four of 40 - 64 behind
+        // 8 192 208, 134 and 132; eight of 16 behind 4 096 128, 56.3 and 58.0; four of 16 64, 27.9 and 29.3; one 16, 40 and 50)
+        if ((int64_t)tiles * 4 >= (int64_t)num_cus() * 3) return launch(tree_join_kernel<DT, D>, dim3(tiles), dim3(kCommonThreads), 0, st, p);
+    }
     return (int64_t)tiles * (D / 32) < num_cus() ? launch(common_join_kernel<DT, D, 16, TREE>, dim3(tiles, D / 16), dim3(kCommonThreads), 0, st, p)
                                                  : launch(common_join_kernel<DT, D, 32, TREE>, dim3(tiles, D / 32), dim3(kCommonThreads), 0, st, p);
 }
