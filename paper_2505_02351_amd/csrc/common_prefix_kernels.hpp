@@ -79,6 +79,7 @@ struct CommonParams {
     const uint32_t* masks;      // [T][mask_words]
     const int32_t* positions;   // [T]
     int mask_words;
+    bool direct;                // TREE: every segment is one piece, and there is no join
 };
 
 template <int D, bool KV8> constexpr int kCommonLds = [] {
@@ -133,6 +134,7 @@ template <bool TREE> struct OwnParts {
     int len, first, rows;       // context length, first token, rows (new tokens x heads of the group)
     int steps, segments;        // of a segment; segments (0: nothing to do)
     int pieces, before;         // of a segment; pieces of all sequences before this one (number())
+    bool alone;                 // there is no prefix
     int row_waves;              // row blocks to a workgroup: 1, 2 or 4
     static __device__ __forceinline__ int row_waves_of(const CommonParams& p, int rows)
     {
@@ -144,6 +146,7 @@ template <bool TREE> struct OwnParts {
     __device__ __forceinline__ OwnParts(const CommonParams& p, int from)
     {
         const int lane = threadIdx.x & 63, b = min(from + lane, p.num_seqs - 1);
+        alone = p.prefix_len == 0;
         len = p.context_lens[b];
         first = p.cu_q_lens ? p.cu_q_lens[b] : b;
         rows = (p.cu_q_lens ? p.cu_q_lens[b + 1] - first : 1) * p.group;
@@ -156,6 +159,10 @@ template <bool TREE> struct OwnParts {
     __device__ __forceinline__ void number(int most, int& all)
     {
         pieces = div_by_inverse(steps + most - 1, most, __builtin_amdgcn_rcpf((float)most));
+        // TREE, no prefix: up to two shares, or four steps more than one, stay one piece, whose workgroup writes the output and leaves nothing to join.  (64 trees
+        // of 16, 24 and 60 behind 1 000 - 2 000, 32 / 8 heads and 64 / 8: 101 -> 77 us, 133 -> 108, 380 -> 341; lines at 1.5 and 2.5 shares: 32 of 16 behind 1 000 - 2 000 68 and
+        // 55, 59 here, 24 52 and 56, 61 here.)
+        if (TREE && alone && steps <= most + max(most, kTreeOneSteps - 1)) pieces = min(pieces, 1);
         const int mine = pieces * segments, sum = lane_sums(mine);
         before = all + sum - mine;
         all += __builtin_amdgcn_readlane(sum, 63);
@@ -193,6 +200,7 @@ struct CommonJob {
     int tok0, pos0;             // token and position of row 0 (pos0: own parts)
     int64_t slot;               // piece of its first 32 rows
     int held_first, held;       // the lane's entry of `table`: held_first + lane
+    bool direct;                // TREE: all keys of its rows: it writes their output
 };
 
 // of 16 bytes of values, or of codes (whose only such value is NaN)
@@ -647,8 +655,20 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
         const int e = 4 * (i & 3);
         return make_float4(a[e], a[e + 1], a[e + 2], a[e + 3]);
     };
+    // (direct: dims 8 piece + 4 h2 .. + 3 of the row's output; a row that sees no key: +0; a sum that is no number stays one)
+    auto write_out = [&](int piece, float4 x, float l) __attribute__((always_inline)) {
+        const float inv = l == 0.f ? 0.f : (p.v_scales ? p.v_scales[job.g] : p.out_scale) / l;
+        uint2 packed;
+        packed.x = l == 0.f ? 0u : narrow2<DT>(x.x * inv, x.y * inv);
+        packed.y = l == 0.f ? 0u : narrow2<DT>(x.z * inv, x.w * inv);
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + ((int64_t)t * p.num_heads + head) * D + 8 * piece + 4 * h2) = packed;
+    };
     if constexpr (KS == 1) {
-        if (row_ok) {
+        if (TREE && job.direct) {
+            if (row_ok)
+#pragma unroll
+                for (int i = 0; i < kPieces; ++i) write_out(i, piece_of(i), l_row);
+        } else if (row_ok) {
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) o[64 * i] = piece_of(i);
             if (h2 == 0) *ml = make_float2(m_row, l_row);
@@ -679,9 +699,11 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
                 const float4 x = xo[((k * RW + rw) * kPieces + piece) * 64 + lane];
                 s.x = fmaf(f[k], x.x, s.x), s.y = fmaf(f[k], x.y, s.y), s.z = fmaf(f[k], x.z, s.z), s.w = fmaf(f[k], x.w, s.w);
             }
-            if (row_ok) o[64 * piece] = s;
+            if (TREE && job.direct) {
+                if (row_ok) write_out(piece, s, l_all);
+            } else if (row_ok) o[64 * piece] = s;
         }
-        if (kw == 0 && h2 == 0 && row_ok) *ml = make_float2(m_all, l_all);
+        if (!(TREE && job.direct) && kw == 0 && h2 == 0 && row_ok) *ml = make_float2(m_all, l_all);
     }
 }
 
@@ -690,8 +712,17 @@ __global__ __launch_bounds__(kCommonThreads, 2) void common_prefix_kernel(const 
 {
     const int lane = threadIdx.x & 63;
     CommonJob job;
-    const int p_workgroups = p.p_items.workgroups();
-    job.prefix = (int)blockIdx.x < p_workgroups;
+    if (TREE && p.direct && (int)blockIdx.x < p.num_tokens) {
+        // a token that no piece has: none of a sequence's, or of one without a context
+        const int t = blockIdx.x;
+        const TokenPlace at = PlaceGuess(p, t).find(p, t);
+        if (at.seq >= 0 && at.len > 0) return;
+        uint32_t* const out = static_cast<uint32_t*>(p.out) + (int64_t)t * p.num_heads * (D / 2);
+        for (int i = threadIdx.x; i < p.num_heads * (D / 2); i += kCommonThreads) out[i] = 0u;
+        return;
+    }
+    const int p_workgroups = TREE && p.direct ? p.num_tokens : p.p_items.workgroups();
+    job.prefix = !(TREE && p.direct) && (int)blockIdx.x < p_workgroups;
     int row_waves = job.prefix ? p.p_row_waves : p.s_row_waves;
     if (job.prefix) {
         int range, tile;
@@ -702,6 +733,7 @@ __global__ __launch_bounds__(kCommonThreads, 2) void common_prefix_kernel(const 
         job.row0 = tile * 32 * row_waves;
         job.num_rows = p.rows;
         job.tok0 = job.pos0 = 0;
+        job.direct = false;
         job.slot = ((int64_t)range * p.num_kv_heads + job.g) * p.p_slots + tile * row_waves;
     } else {
         const int me = blockIdx.x - p_workgroups;              // the piece
@@ -721,6 +753,7 @@ __global__ __launch_bounds__(kCommonThreads, 2) void common_prefix_kernel(const 
         const int pieces = __builtin_amdgcn_readlane(parts.pieces, l), in_seq = me - __builtin_amdgcn_readlane(parts.before, l);
         const int segment = __builtin_amdgcn_readfirstlane(in_seq / pieces), each = __builtin_amdgcn_readfirstlane(Own::each(steps, pieces));
         if (TREE) row_waves = __builtin_amdgcn_readlane(parts.row_waves, l);
+        job.direct = TREE && p.prefix_len == 0 && pieces == 1;
         const int lo = (in_seq - segment * pieces) * each, hi = min(lo + each, steps);
         if (hi <= lo) return;                                    // (equal pieces of, say, 7 steps in 4: the last is empty)
         job.num_rows = __builtin_amdgcn_readlane(parts.rows, l);
@@ -797,6 +830,7 @@ template <int J> struct JoinState {
 // A row's pieces of its sequence's own part: the steps in which it sees a key, and the workgroups that had them.
 template <bool TREE> struct OwnPieces {
     int count = 0, row_off = 0;         // how many; how far its row in them lies from row n32
+    bool written = false;               // TREE: the only piece of all has written the row's output
     int64_t first = 0;
     __device__ __forceinline__ OwnPieces(const CommonParams& p, const PlaceGuess& guess, OwnParts<TREE>& parts, int t, int g, int rc, int n32)
     {
@@ -816,6 +850,8 @@ template <bool TREE> struct OwnPieces {
                 const int tiles = ((at.end - at.first) * p.group + tile_rows - 1) >> tile_shift;
                 const int each = Own::each(steps, pieces);
                 count = div_by_inverse(Own::steps_of(waves, behind) + each - 1, each, __builtin_amdgcn_rcpf((float)each));
+                written = TREE && p.prefix_len == 0 && pieces == 1;
+                if (written) count = 0;
                 row_off = (in_seq & 31) - n32;
                 first = p.s_first + (int64_t)(before + (g * tiles + (in_seq >> tile_shift)) * pieces) * p.s_row_waves + ((in_seq >> 5) & (waves - 1));
             }
@@ -850,6 +886,7 @@ __global__ __launch_bounds__(kCommonThreads) void common_join_kernel(const Commo
     };
     prefix.load(p, o, n32, wave, p.p_splits, prefix_at);
     const OwnPieces<TREE> mine(p, guess, parts, t, g, rc, n32);
+    if (TREE && __builtin_amdgcn_ballot_w64(!mine.written) == 0) return;         // (all waves alike)
     const int n = mine.count;
     auto own_at = [&](int i, int& row) __attribute__((always_inline)) {
         row = mine.row_off;
@@ -887,7 +924,7 @@ __global__ __launch_bounds__(kCommonThreads) void common_join_kernel(const Commo
         l_all = fmaf(f, t2.y, l_all);
         s.x = fmaf(f, x.x, s.x), s.y = fmaf(f, x.y, s.y), s.z = fmaf(f, x.z, s.z), s.w = fmaf(f, x.w, s.w);
     }
-    if (r >= p.rows) return;
+    if (r >= p.rows || (TREE && mine.written)) return;
     // (a row that sees no key: +0; a sum that is no number stays one)
     const float inv = l_all == 0.f ? 0.f : (p.v_scales ? p.v_scales[g] : p.out_scale) / l_all;
     uint2 packed;
@@ -929,7 +966,7 @@ __global__ __launch_bounds__(kCommonThreads) void tree_join_kernel(const CommonP
         own.load(p, o, n32, i0, mine.count, own_at);
         state.add(own);
     }
-    if (r >= p.rows) return;
+    if (r >= p.rows || mine.written) return;
     // (a row that sees no key: +0; a sum that is no number stays one)
     const float inv = state.l == 0.f ? 0.f : (p.v_scales ? p.v_scales[g] : p.out_scale) / state.l;
     uint16_t* const to = static_cast<uint16_t*>(p.out) + ((int64_t)t * p.num_heads + head) * D + wave * (8 * J) + 4 * h2;

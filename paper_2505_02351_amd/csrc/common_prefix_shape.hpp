@@ -40,6 +40,7 @@ struct CommonPlan {
     int p_row_waves, p_tiles, p_splits, p_keys, s_row_waves, s_shares;
     int64_t rows, p_slots, p_units, s_workgroups;                // s_workgroups: own pieces at most
     int64_t held;                                                // pieces of 32 rows that the workspace has to hold
+    int64_t direct_workgroups;                                   // trees: more than 0: no join; a workgroup to a token and a piece
     int64_t p_pieces(int num_kv_heads) const { return num_kv_heads * p_splits * p_slots; }
     int64_t workgroups() const { return (p_units * p_tiles + kCommonXcds - 1) / kCommonXcds * kCommonXcds + s_workgroups; }
     int64_t pieces(int num_kv_heads) const { return p_pieces(num_kv_heads) + s_workgroups * s_row_waves; }
@@ -71,6 +72,12 @@ inline int64_t tree_ranges(int64_t units, int64_t steps, int64_t slots, int64_t 
 // workgroups to each, and with one as much of that as their steps are of all.  (1, 2, 3, 4 and 6 to a CU: two trees of 64 behind 32 000, 64 / 8 heads, the first launch alone, 323, 214, 222, 207 and 199 us; with the
 // join 206 at 2, 217 at 3, 212 at 4.  64 trees of 12 - 24 behind 511 - 2 047, 32 / 8, 110, 111 and 114 at 2, 3 and 4.)
 inline int64_t common_most_shares(int64_t cus, bool alone) { return std::max<int64_t>(alone ? 2 * cus : cus / 2, 1); }
+
+// Trees with no prefix whose segments have so many steps at most are one piece each, whatever the shares; the call is one launch then, that writes the
+// output.  (A replayed graph's call, us, of one and of two launches: one tree of 8, 8 / 2 heads of 64, behind 120 tokens 6.8 and 10.4, 500 (4 steps) 8.4 and 10.5,
+// 1 000 11.9 and 10.7; one of 16, 32 / 8 heads of 128, 250 (4 steps) 11.8 and 13.2, 500 16.7 and 13.4; eight of those 250 14.0 and 17.3, 500 17.5 and 22.1, 1 000
+// 26.9 and 24.5.)
+constexpr int kTreeOneSteps = 5;
 
 // Pieces that any call has that is no larger in its tokens, sequences, prefix, longest context and new tokens of a sequence: what is
 // held for a call serves all smaller ones.  (The pieces of the calls themselves go up and down: a workgroup's worth of rows more
@@ -138,6 +145,9 @@ inline bool plan_common(CommonPlan& c, int64_t num_tokens, int64_t num_seqs, int
         // no more than the shares and one for each segment
         c.s_workgroups = c.s_shares + num_kv_heads * (c.rows / tile_rows + num_seqs);
     }
+    if (tree && prefix_len == 0 && (max_context_len + 32 * (kCommonWaves / c.s_row_waves) - 1) / (32 * (kCommonWaves / c.s_row_waves)) <= kTreeOneSteps &&
+        num_tokens + c.s_workgroups <= kCommonMostWorkgroups)
+        c.direct_workgroups = num_tokens + c.s_workgroups;
     if (c.workgroups() > kCommonMostWorkgroups) return false;
     c.held = common_held(c.rows, num_seqs, own_rows, num_kv_heads, prefix_len, max_context_len, cus, common_most_shares(cus, tree), tree);
     return true;

@@ -185,6 +185,7 @@ int launch_common(const CommonParams& p, int workgroups, hipStream_t st)
     // tokens: 16.0 us against 16.4; 32 of 3 - 6 new tokens each, 40 / 8 heads: 47.1 against 44.9)
     const int tiles = p.p_slots * p.num_kv_heads;
     if constexpr (TREE) {
+        if (p.direct) return OPTGQA_OK;
         // all dims to a workgroup where those are three to four CUs or more: the rows have few pieces then (replayed graphs, us, so many of 32 rows, without and with: 64 trees
         // of 12 - 24 behind 511 - 2 047 1 160, 111 and 101; 64 of 8 - 24 behind 4 096 1 024, 144 and 132; two of 64 behind 32 000 256, 204 and 204; four of 40 - 64 behind
         // 8 192 208, 134 and 132; eight of 16 behind 4 096 128, 56.3 and 58.0; four of 16 64, 27.9 and 29.3; one 16, 40 and 50)
@@ -293,7 +294,8 @@ int common_impl(void* out, const void* q, const void* k_cache, const void* v_cac
     p.positions = tree && alibi_slopes ? tree->positions : nullptr;
     p.mask_words = tree ? tree->words : 0;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const int workgroups = (int)c.workgroups();
+    p.direct = c.direct_workgroups > 0;
+    const int workgroups = (int)(p.direct ? c.direct_workgroups : c.workgroups());
     return tree ? launch_common_t<true>(p, dtype, scales != nullptr, head_dim, workgroups, st)
                 : launch_common_t<false>(p, dtype, scales != nullptr, head_dim, workgroups, st);
 }
