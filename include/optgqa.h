@@ -751,6 +751,7 @@ int optgqa_verify_drafts(int64_t *tokens, int32_t *num_accepted, const void *tar
  *   copies          [num_seqs][2] int32: the pairs, in order of their sequences.  They have to be copied before the new tokens are stored
  *   counts          [2] int32: the number of pairs; blocks that were lacking (0: all sequences have their lengths)
  *   max_change      an upper bound on |new length - old length|; it sizes the launch (a change beyond it is made all the same)
+ *   num_seqs, max_blocks_per_seq   num_seqs * (max_blocks_per_seq + 1) below 2^31 (OPTGQA_ERR_SHAPE)
  *   workspace       optgqa_resize_workspace_bytes(...) bytes, 16-byte aligned (OPTGQA_ERR_WORKSPACE without it)
  *
  * optgqa_fork_sequences: row i of tables_out [num_out][max_blocks_per_seq] and lens_out becomes row parents[i] of the old table, all of them
@@ -772,7 +773,8 @@ int optgqa_verify_drafts(int64_t *tokens, int32_t *num_accepted, const void *tar
  *
  * optgqa_keep_tokens: of the tokens behind position start_lens[b] - a tree of drafts, optgqa_paged_attention_tree - those on the accepted
  * branch come to the front: in all caches the row at start_lens[b] + paths[b][i] goes to start_lens[b] + i, for i <
- * path_lens[b].  paths[b] ascends strictly.  Other rows keep their bits (cut the sequence to start_lens[b] + path_lens[b] afterwards).
+ * path_lens[b].  paths[b] ascends strictly.  Other rows keep their bits (cut the sequence to start_lens[b] + path_lens[b] afterwards).  The blocks of
+ * these rows have to be the sequence's alone, as they are after the resize that made room for the tree.
  *   paths           [num_seqs][max_path] int32;   num_seqs at most 65 535
  *   element_bytes   2, or 1 for 8-bit caches
  */

@@ -26,6 +26,12 @@ bool tables_ok(int num_seqs, int max_blocks_per_seq, int num_blocks)
     return num_seqs >= 0 && max_blocks_per_seq > 0 && num_blocks > 0 && num_seqs <= most_workgroups(kPageThreads);
 }
 
+// a resize counts the blocks that all rows ask for in 32 bits
+bool resize_ok(int num_seqs, int max_blocks_per_seq, int num_blocks)
+{
+    return tables_ok(num_seqs, max_blocks_per_seq, num_blocks) && (int64_t)num_seqs * ((int64_t)max_blocks_per_seq + 1) < (1ll << 31);
+}
+
 // workgroups of kPageThreads for the entries of a table's row, `each` a workgroup
 unsigned row_parts(int64_t entries, int each) { return (unsigned)std::min<int64_t>(std::max<int64_t>((entries + each - 1) / each, 1), 65535); }
 
@@ -107,7 +113,7 @@ int optgqa_fork_sequences(int32_t* tables_out, int32_t* lens_out, const int32_t*
 
 size_t optgqa_resize_workspace_bytes(int num_seqs, int max_blocks_per_seq, int num_blocks)
 {
-    if (num_seqs <= 0 || !tables_ok(num_seqs, max_blocks_per_seq, num_blocks)) return 0;
+    if (num_seqs <= 0 || !resize_ok(num_seqs, max_blocks_per_seq, num_blocks)) return 0;
     // three numbers a row, and every block that the rows could ask for
     return 4 * (3 * (size_t)num_seqs + (size_t)std::min<int64_t>(num_blocks, (int64_t)num_seqs * ((int64_t)max_blocks_per_seq + 1)));
 }
@@ -116,7 +122,7 @@ int optgqa_resize_sequences(int32_t* block_tables, int32_t* context_lens, int32_
                             const int32_t* cu_new_lens, int32_t* copies, int32_t* counts, int num_seqs, int max_blocks_per_seq, int num_blocks,
                             int block_size, int num_slots, int max_change, void* workspace, size_t workspace_bytes, void* stream)
 {
-    if (!tables_ok(num_seqs, max_blocks_per_seq, num_blocks) || num_slots < 0 || max_change < 0) return OPTGQA_ERR_SHAPE;
+    if (!resize_ok(num_seqs, max_blocks_per_seq, num_blocks) || num_slots < 0 || max_change < 0) return OPTGQA_ERR_SHAPE;
     if (!block_size_ok(block_size)) return OPTGQA_ERR_UNSUPPORTED;
     if (!counts || (num_seqs && (!block_tables || !context_lens || !ref_counts || !new_lens || !copies || (slot_mapping && !cu_new_lens))))
         return OPTGQA_ERR_NULL;

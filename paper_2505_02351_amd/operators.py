@@ -87,6 +87,15 @@ def _dense(*tensors) -> None:
             raise ValueError(f"optgqa: {name} must be contiguous")
 
 
+# (a private name, as for _stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _here(index: int) -> None:
+    if _current_device() != index:
+        raise ValueError(f"optgqa: the tensors are on GPU {index}, which is not the current one")
+
+
 def _rows(t: torch.Tensor, name: str, tokens: int, D: int) -> Tuple[int, int]:
     """(heads, token stride) of a [T, heads, D] tensor whose tokens' rows are dense."""
     shape = t.shape
@@ -228,8 +237,7 @@ def _common(name, out, q, k_cache, v_cache, prefix_table, block_tables, context_
         if len(shape) != 2 or shape[0] != T or (tree[1] is not None and tree[1].shape != (T,)):
             raise ValueError("optgqa: shape mismatch between q, tree_masks and positions")
         _dense(*((t, name) for t, name in zip(tree, ("tree_masks", "positions")) if t is not None))
-        if torch._C._cuda_getDevice() != index:
-            raise ValueError(f"optgqa: the tensors are on GPU {index}, which is not the current one")
+        _here(index)
         masks, words = (tree[0].data_ptr(), _pkg._ptr(tree[1])), (shape[1],)
     ws_bytes = _pkg._workspace(workspace, q)
     rc = getattr(lib, name)(out.data_ptr(), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), prefix_table.data_ptr(),

@@ -13,7 +13,7 @@ import torch
 
 import paper_2505_02351_amd as _pkg
 
-from .operators import _check_tensors, _dense
+from .operators import _check_tensors, _dense, _here
 
 
 def declare(lib: ctypes.CDLL) -> None:
@@ -63,9 +63,6 @@ def _cache_set(caches) -> CacheSet:
     return caches
 
 
-def _here(index: int) -> None:
-    if torch._C._cuda_getDevice() != index:
-        raise ValueError(f"optgqa: the tensors are on GPU {index}, which is not the current one")
 
 
 def _pool(block_tables, context_lens, ref_counts):

@@ -128,6 +128,22 @@ def test_the_lowest_free_blocks_of_a_large_pool(G, NB):
     same(resize(G, tables, lens, refs, new, [0, 0], 0, 16), P.resize(tables, lens, refs, new, [0, 0], 0, 16))
 
 
+@pytest.mark.parametrize("hint", [0, 1 << 20])
+def test_thousands_of_new_blocks(G, hint):
+    """More new blocks than a plan holds in LDS, given to few rows; some of them shared, some lacking none."""
+    bs, M = 16, 1500
+    rng = np.random.RandomState(7)
+    tables, lens, refs = P.pool(rng, 6, M, bs, 50, 0.5)
+    lens, refs = np.minimum(lens, 1000).astype(np.int32), np.zeros_like(refs)
+    for row, n in zip(tables, lens):
+        np.add.at(refs, row[:P.have(n, bs)], 1)
+    new = np.full(6, M * bs - 5)
+    cu = np.concatenate([[0], np.cumsum(new - lens)])
+    want = P.resize(tables, lens, refs, new, cu, int(cu[-1]), bs)
+    assert want[5] == 0 and len(np.flatnonzero(want[2] != refs)) > 4096
+    same(resize(G, tables, lens, refs, new, cu, int(cu[-1]), bs, hint), want)
+
+
 @pytest.mark.parametrize("B,N,M,bs", [(1, 1, 1, 16), (3, 8, 5, 16), (64, 40, 9, 32), (300, 300, 3, 64), (2, 3, 2500, 16)])
 def test_fork(G, B, N, M, bs):
     import torch

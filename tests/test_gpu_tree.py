@@ -180,6 +180,24 @@ def test_rows_that_see_nothing(G):  # noqa: F811
         assert (got[i].view(dtype=__import__("torch").int16) == 0).all()
 
 
+@pytest.mark.parametrize("bound", [0, 9000])
+@pytest.mark.parametrize("kv8", [False, True])
+def test_contexts_that_hold_only_the_last_of_the_new_tokens(G, bound, kv8):  # noqa: F811
+    """Lengths below the number of new tokens: those that lie in front of the first row are not there; none at all: +0.  Under a tight bound
+    (one launch) and a wide one (two)."""
+    t = Trees(13, "bf16", 16, 4, 64, 16, 0, [3, 0, 40, 1, 31], [5, 4, 40, 33, 0], slopes=True, kv8=kv8, pad_tokens=2).upload()
+    t.check(t.run(G, bounds=(bound, 0)))
+
+
+@pytest.mark.parametrize("NP", [0, 2])
+def test_a_batch_of_long_and_short_ones(G, NP):  # noqa: F811
+    """Sequences of one piece, which write their output, beside some of several, in one row block of the join."""
+    lens, new = [700 if b % 5 == 3 else 40 + b for b in range(20)], [1 + b % 4 for b in range(20)]
+    lens[7], new[11] = 6000, 0
+    t = Trees(14, "f16", 8, 2, 64, 16, NP, lens, new, slopes=True, pad_tokens=1).upload()
+    t.check(t.run(G))
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 def test_one_new_token_each(G, dtype):  # noqa: F811
     """A decode step: no prefix sums; tokens that see themselves and one that does not."""

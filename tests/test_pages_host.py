@@ -39,7 +39,9 @@ def test_resize_refuses(G):
     assert need >= 4 * (3 * 3 + 10)
     assert call(ws=None) == -4 and call(ws_bytes=need - 1) == -4 and call(ws=ctypes.c_void_p(24)) == -4
     assert G.resize_workspace_bytes(0, 4, 10) == 0 and G.resize_workspace_bytes(3, 0, 10) == 0 and G.resize_workspace_bytes(3, 4, 0) == 0
-    assert G.resize_workspace_bytes(1 << 20, 1 << 20, 1 << 30) == 4 * (3 * (1 << 20) + (1 << 30))
+    assert G.resize_workspace_bytes(1 << 10, (1 << 21) - 2, 1 << 30) == 4 * (3 * (1 << 10) + (1 << 30))
+    # blocks that all rows could ask for, counted in 32 bits
+    assert G.resize_workspace_bytes(1 << 10, (1 << 21) - 1, 1 << 30) == 0 and call(S=1 << 10, M=(1 << 21) - 1, ws_bytes=1 << 40) == -2
 
 
 def test_fork_refuses(G):
