@@ -183,8 +183,8 @@ int optgqa_compact_blocks(int32_t* block_tables, const int32_t* context_lens, in
     p.num_blocks = num_blocks;
     p.block_shift = __builtin_ctz(block_size);
     p.max_copies = max_copies;
-    // (a graph's call and a direct one, us, one launch and two: 5 rows of up to 12 blocks 3.6 and 4.7, 6.5 and 8.7; 64 of 95 5.4 and 5.3, 6.3 and 8.7; 64
-    // of 250 7.8 and 6.8, 7.5 and 8.6; 16 of 1 000 6.7 and 6.1, 6.4 and 8.6)
+    // (a graph's call and a direct one, us, one launch and two: 5 rows of up to 12 blocks 3.4 and 4.7, 6.6 and 8.7; 64 of 95 4.8 and 5.3, 6.5 and 8.7; with a wave to a
+    // row, not 16 threads, 64 of 250 7.8 and 6.8, 7.5 and 8.6, 16 of 1 000 6.7 and 6.1, 6.4 and 8.6)
     p.tables_too = num_seqs <= 4 * kPlanWaves && (int64_t)num_seqs * max_blocks_per_seq <= 8192;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int rc = launch(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, p);
