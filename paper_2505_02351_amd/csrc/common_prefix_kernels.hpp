@@ -575,6 +575,9 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
             if (kLead > 1 && (decltype(inner)::value || j + kLead < mine)) wait_direct<(kLead - 1) * kLoads>();
             else wait_direct();
             __syncthreads();                                     // ... for all; and the buffers read in step j - 1 are free
+            // (TREE: the matrix instructions of the scores go before what the SIMD's other wave has to do: two trees of 64 behind 32 000 208 -> 202 us; before
+            // those of the output 203, E4M3 136 -> 138; before the softmax 211, 141)
+            if (TREE) __builtin_amdgcn_s_setprio(1);
             st_ahead = scores(buffer(j + 1), [&]() __attribute__((always_inline)) {
                 if (decltype(inner)::value) {
                     const At at = at_of(j + 1 + kLead);
@@ -586,6 +589,7 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
                     ask_v(j + kLead);
                 }
             });
+            if (TREE) __builtin_amdgcn_s_setprio(0);
             if (!decltype(masked)::value || j < mine) finish(j, st_cur, buffer_v(j), masked);
         };
         f32x16 st, st_other;
