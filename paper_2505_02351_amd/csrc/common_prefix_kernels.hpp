@@ -22,6 +22,11 @@
 // one after another, short launches by their chains of loads.  Measured (both launches, inputs in turn): 64 sequences, 32 / 8 heads of 128, bf16, behind
 // 32 768 tokens, 1 023 - 2 047 own: 108 - 110 us, 5.0 TB/s; 32 / 4 heads behind 4 096, 127 - 1 023 own, slopes: 30 - 31; 16 of 2 - 9 drafts, 64 / 8 heads,
 // fp16, behind 8 192: 44.6 us, 480 TFLOP/s; 32 behind 8 192, E4M3 caches: 27.6 - 28.3.
+// TREE: the new tokens' keys are seen by masks, one bit for each of the sequence's new tokens, which tiles behind the context look up (two words of the row's
+// mask and a shift make a tile's 32 bits); everything in front of them is seen by all rows and needs none.  Without a prefix the own parts have the CUs to themselves, two
+// workgroups to each, and a segment that is one piece writes its output.  Bound by memory while rows are few (64 trees of 12 - 24 behind 511 - 2 047, 32 / 8 heads,
+// bf16, slopes: 90 - 98 us, 328 MB; 5.5 TB/s but for the pieces that end last), by matrix and vector instructions where they are many (two trees of 64 behind 32 000, 64 / 8,
+// bf16: 191 - 202 us, 670 - 710 TFLOP/s, over 1 000 with the weights' second half; 16 of 20 - 60 behind a common 8 192, 32 / 4, fp16, E4M3: 121 us, 820).
 // (head_dim 128 with bf16 takes all 256 registers that two workgroups to a CU leave a wave, and one more, which lies in scratch.)
 #pragma once
 #include <type_traits>
