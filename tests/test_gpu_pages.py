@@ -255,6 +255,28 @@ def test_keep_tokens(G, dtype, n, Hkv, bs, D, B, nodes, longest):
         assert (bits_of(t) == w).all()
 
 
+def test_rows_beyond_4_gib(G):
+    """A cache of more than 2^32 bytes: blocks are copied and rows moved at both of its ends."""
+    import torch
+    NB, Hkv, bs, D = 70000, 4, 64, 128
+    cache = torch.empty(NB, Hkv, bs, D, dtype=torch.float16, device="cuda")
+    assert cache.numel() * 2 > 1 << 32
+    gen = torch.Generator("cuda").manual_seed(1)
+    used = [0, 1, NB - 1, NB - 2, 33000]
+    for b in used:
+        cache[b] = torch.randn(Hkv, bs, D, generator=gen, device="cuda").half()
+    before = {b: cache[b].clone() for b in used}
+    s = G.CacheSet([cache])
+    G.copy_blocks(s, dev([[0, NB - 1], [NB - 2, 1]]), dev([2]))
+    assert torch.equal(cache[NB - 1], before[0]) and torch.equal(cache[1], before[NB - 2]) and torch.equal(cache[33000], before[33000])
+    # rows 60 and 66 of a sequence whose blocks lie at either end
+    first, last = cache[NB - 1].clone(), cache[33000].clone()
+    G.keep_tokens(s, dev([[NB - 1, 33000]]), dev([10]), dev([[0, 50, 56]]), dev([3]))
+    want = first.clone()
+    want[:, 11], want[:, 12] = first[:, 60], last[:, 2]
+    assert torch.equal(cache[NB - 1], want) and torch.equal(cache[33000], last) and torch.equal(cache[0], before[0])
+
+
 def test_keep_tokens_passes_over_what_is_nowhere(G):
     import torch
     tables = np.array([[0, 1], [7, 2], [3, 99]])
