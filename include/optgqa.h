@@ -746,7 +746,8 @@ int optgqa_verify_drafts(int64_t *tokens, int32_t *num_accepted, const void *tar
  * sequence grows, and shorter ones are cut all the same.
  *   slot_mapping    [num_slots] int64 or NULL: where the new tokens go, token i of sequence b (position old length + i) at
  *                   slot_mapping[cu_new_lens[b] + i]; -1 for those of a sequence's cu_new_lens[b + 1] - cu_new_lens[b] that it
- *                   did not grow by (the cache stores pass over such slots).  Slots from cu_new_lens[num_seqs] on are left
+ *                   did not grow by and where the last block's entry names none (the cache stores pass over such slots).  Slots from
+ *                   cu_new_lens[num_seqs] on are left
  *   cu_new_lens     [num_seqs + 1] int32 prefix sums (NULL where slot_mapping is)
  *   copies          [num_seqs][2] int32: the pairs, in order of their sequences.  They have to be copied before the new tokens are stored
  *   counts          [2] int32: the number of pairs; blocks that were lacking (0: all sequences have their lengths)

@@ -1,0 +1,45 @@
+"""CPU: the slots that a resize gives to a sequence's new tokens never name a row outside of the pool."""
+import ctypes
+import os
+import subprocess
+
+import numpy as np
+import pytest
+
+import common_prefix_plan as P
+
+
+@pytest.fixture(scope="module")
+def apply(tmp_path_factory):
+    out = str(tmp_path_factory.mktemp("pages") / "libpages.so")
+    subprocess.run([os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "llvm", "bin", "clang++"), "-std=c++17", "-O1", "-fPIC", "-shared", "-Wno-ignored-attributes",
+                    "-I" + os.path.join(P.HERE, "host_hip"), "-I" + P.CSRC, os.path.join(P.HERE, "host_hip", "pages.cpp"), "-o", out], check=True)
+    f, vp, i32 = ctypes.CDLL(out).resize_apply_of, ctypes.c_void_p, ctypes.c_int
+    f.restype, f.argtypes = None, [vp, vp, vp, i32, vp, vp] + [i32] * 6 + [vp, i32, i32]
+
+    def run(row, old, new, last, fresh, cu, num_slots, num_blocks, bs=16, enough=True, step=1):
+        """(row, length, slots): -2 where nothing was written."""
+        length, refs = np.array([old], np.int32), np.zeros(num_blocks, np.int32)
+        slots, cu, fresh = np.full(num_slots, -2, np.int64), np.array(cu, np.int32), np.array([*fresh, -9], np.int32)
+        f(row.ctypes.data, length.ctypes.data, refs.ctypes.data, new, slots.ctypes.data, cu.ctypes.data, num_slots, row.shape[0], num_blocks,
+          bs.bit_length() - 1, old, last, fresh.ctypes.data, int(enough), step)
+        return row, int(length[0]), slots
+
+    return run
+
+
+@pytest.mark.parametrize("step", [1, 3])
+@pytest.mark.parametrize("bad", [-1, -7, 30, 31, 1 << 28, 2 ** 31 - 1, -2 ** 31])
+def test_tokens_of_a_last_block_that_is_none(apply, bad, step):
+    """A row of 20 tokens whose second entry names no block grows to 37: tokens 20 .. 31 have no row, 32 .. 36 lie in its new block."""
+    row, length, slots = apply(np.array([5, bad, -7, -7], np.int32), 20, 37, -1, [8], [0, 17], 19, 30, step=step)
+    assert row.tolist() == [5, bad, 8, -7] and length == 37
+    assert slots.tolist() == [-1] * 12 + [8 * 16 + i for i in range(5)] + [-2, -2]
+
+
+def test_tokens_of_a_last_block_that_is_one(apply):
+    assert apply(np.array([5, 29, -7], np.int32), 20, 37, -1, [8], [0, 18], 18, 30)[2].tolist() == [29 * 16 + i for i in range(4, 16)] + [128 + i for i in range(5)] + [-1]
+    # replaced: held by others too
+    row, _, slots = apply(np.array([5, 29, -7], np.int32), 20, 37, 29, [2, 8], [0, 17], 17, 30)
+    assert row.tolist() == [5, 2, 8] and slots.tolist() == [2 * 16 + i for i in range(4, 16)] + [128 + i for i in range(5)]
+    assert apply(np.array([5, 29, -7], np.int32), 20, 37, -1, [], [0, 17], 17, 30, enough=False)[1:][1].tolist() == [-1] * 17
