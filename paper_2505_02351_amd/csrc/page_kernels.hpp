@@ -284,10 +284,14 @@ __device__ __forceinline__ void resize_apply(const ResizeParams& p, const Resize
     // of the first tokens, where they fill a block (an entry that names none: they have no row, whatever the cache stores check)
     int kept = grows && have > 0 && (old >> shift) == have - 1 ? row[have - 1] : 0;
     if ((uint32_t)kept >= (uint32_t)p.num_blocks) kept = -1;
+    const int grown = grows ? now - old : 0;                     // (lengths go up to 2^31 - 1, positions behind them would not)
     for (int i = from; i < end - begin; i += step) {
-        const int pos = old + i, j = pos >> shift;
-        const int block = grows && pos < now ? (j < have ? kept : fresh[j - have]) : -1;
-        p.slots[begin + i] = block >= 0 ? ((int64_t)block << shift) + (pos & ((1 << shift) - 1)) : -1;
+        int64_t slot = -1;
+        if (i < grown) {
+            const int pos = old + i, j = pos >> shift, block = j < have ? kept : fresh[j - have];
+            if (block >= 0) slot = ((int64_t)block << shift) + (pos & ((1 << shift) - 1));
+        }
+        p.slots[begin + i] = slot;
     }
 }
 

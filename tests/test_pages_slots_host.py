@@ -12,7 +12,7 @@ import common_prefix_plan as P
 @pytest.fixture(scope="module")
 def apply(tmp_path_factory):
     out = str(tmp_path_factory.mktemp("pages") / "libpages.so")
-    subprocess.run([os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "llvm", "bin", "clang++"), "-std=c++17", "-O1", "-fPIC", "-shared", "-Wno-ignored-attributes",
+    subprocess.run([os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "llvm", "bin", "clang++"), "-std=c++17", "-O1", "-fwrapv", "-fPIC", "-shared", "-Wno-ignored-attributes",
                     "-I" + os.path.join(P.HERE, "host_hip"), "-I" + P.CSRC, os.path.join(P.HERE, "host_hip", "pages.cpp"), "-o", out], check=True)
     f, vp, i32 = ctypes.CDLL(out).resize_apply_of, ctypes.c_void_p, ctypes.c_int
     f.restype, f.argtypes = None, [vp, vp, vp, i32, vp, vp] + [i32] * 6 + [vp, i32, i32]
@@ -43,3 +43,13 @@ def test_tokens_of_a_last_block_that_is_one(apply):
     row, _, slots = apply(np.array([5, 29, -7], np.int32), 20, 37, 29, [2, 8], [0, 17], 17, 30)
     assert row.tolist() == [5, 2, 8] and slots.tolist() == [2 * 16 + i for i in range(4, 16)] + [128 + i for i in range(5)]
     assert apply(np.array([5, 29, -7], np.int32), 20, 37, -1, [], [0, 17], 17, 30, enough=False)[1:][1].tolist() == [-1] * 17
+
+
+def test_more_slots_than_tokens_at_the_longest_length(apply):
+    """Places behind a sequence's new tokens are -1 also where a token there would have a position beyond 2^31."""
+    bs, old, new = 16, 2 ** 31 - 20, 2 ** 31 - 2
+    row = np.zeros(2 ** 27, np.int32)                        # (pages that nobody touches take no memory)
+    row[-2] = 3
+    slots = apply(row, old, new, -1, [7], [0, 60], 60, 30)[2]
+    want = [3 * 16 + i for i in range(12, 16)] + [7 * 16 + i for i in range(14)]
+    assert slots.tolist() == want + [-1] * (60 - len(want))
