@@ -53,3 +53,9 @@ def test_more_slots_than_tokens_at_the_longest_length(apply):
     slots = apply(row, old, new, -1, [7], [0, 60], 60, 30)[2]
     want = [3 * 16 + i for i in range(12, 16)] + [7 * 16 + i for i in range(14)]
     assert slots.tolist() == want + [-1] * (60 - len(want))
+
+
+@pytest.mark.parametrize("cu", [[2 ** 31 - 1, -2 ** 31], [2 ** 31 - 1, -9], [-2 ** 31, -2 ** 31], [2 ** 31 - 1, 2 ** 31 - 1], [40, 2 ** 31 - 1], [19, 0]])
+def test_prefix_sums_that_are_none_write_no_slot(apply, cu):
+    """Room for 19 tokens, prefix sums outside of it."""
+    assert (apply(np.array([5, 29, -7], np.int32), 20, 37, -1, [8], cu, 19, 30)[2] == -2).all()
