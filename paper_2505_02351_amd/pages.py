@@ -7,7 +7,7 @@ block).  All of it stays on the GPU; caches of all layers are handed over as a C
 from __future__ import annotations
 
 import ctypes
-from typing import List, Optional, Sequence
+from typing import Optional, Sequence, Tuple
 
 import torch
 
@@ -37,7 +37,7 @@ class CacheSet:
     caches are (not under graph capture), and kept as long as they are."""
 
     def __init__(self, caches: Sequence[torch.Tensor]):
-        self.caches: List[torch.Tensor] = list(caches)
+        self.caches: Tuple[torch.Tensor, ...] = tuple(caches)
         if not self.caches:
             raise ValueError("optgqa: a CacheSet needs at least one cache")
         for i, t in enumerate(self.caches):
@@ -55,14 +55,13 @@ class CacheSet:
                 raise ValueError(f"optgqa: cache {i} must lie on 16 bytes")
         self.shape, self.element_bytes, self.index = first.shape, first.element_size(), first.get_device()
         self.pointers = torch.tensor([t.data_ptr() for t in self.caches], dtype=torch.int64, device=first.device)
+        self.count = len(self.caches)                            # (of addresses: what the kernels go by)
 
 
 def _cache_set(caches) -> CacheSet:
     if not isinstance(caches, CacheSet):
         raise TypeError(f"optgqa: caches must be a CacheSet, got {type(caches).__name__}")
     return caches
-
-
 
 
 def _pool(block_tables, context_lens, ref_counts):
@@ -160,7 +159,7 @@ def copy_blocks(caches: CacheSet, copies: torch.Tensor, num_copies: torch.Tensor
     _dense((copies, "copies"), (num_copies, "num_copies"))
     _here(s.index)
     NB, Hkv, bs, D = s.shape
-    rc = lib.optgqa_copy_blocks(s.pointers.data_ptr(), len(s.caches), copies.data_ptr(), num_copies.data_ptr(), copies.shape[0], NB,
+    rc = lib.optgqa_copy_blocks(s.pointers.data_ptr(), s.count, copies.data_ptr(), num_copies.data_ptr(), copies.shape[0], NB,
                                 Hkv * bs * D * s.element_bytes, _pkg._stream(stream))
     if rc:
         _pkg._check(rc, "optgqa_copy_blocks")
@@ -179,7 +178,7 @@ def keep_tokens(caches: CacheSet, block_tables: torch.Tensor, start_lens: torch.
     _dense((block_tables, "block_tables"), (start_lens, "start_lens"), (paths, "paths"), (path_lens, "path_lens"))
     _here(s.index)
     NB, Hkv, bs, D = s.shape
-    rc = lib.optgqa_keep_tokens(s.pointers.data_ptr(), len(s.caches), block_tables.data_ptr(), start_lens.data_ptr(), paths.data_ptr(),
+    rc = lib.optgqa_keep_tokens(s.pointers.data_ptr(), s.count, block_tables.data_ptr(), start_lens.data_ptr(), paths.data_ptr(),
                                 path_lens.data_ptr(), tables[0], places[1], tables[1], NB, Hkv, D, bs, s.element_bytes, _pkg._stream(stream))
     if rc:
         _pkg._check(rc, "optgqa_keep_tokens")
