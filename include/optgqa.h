@@ -769,7 +769,7 @@ int optgqa_verify_drafts(int64_t *tokens, int32_t *num_accepted, const void *tar
  * optgqa_copy_blocks: for the first *num_copies (at most max_copies) pairs (from, to) block `to` of every cache becomes a copy of block
  * `from`.  No block may be written by one pair and read or written by another (the calls above make no such pairs).
  *   caches          [num_caches] device pointers, in device memory: K and V caches of all layers, each num_blocks blocks of
- *                   block_bytes (a multiple of 16), 16-byte aligned
+ *                   block_bytes (a multiple of 16), 16-byte aligned; no two of them may overlap, or be the same
  *   num_copies      device, e.g. counts of the calls above
  *
  * optgqa_keep_tokens: of the tokens behind position start_lens[b] - a tree of drafts, optgqa_paged_attention_tree - those on the accepted

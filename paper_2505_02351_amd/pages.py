@@ -7,7 +7,7 @@ block).  All of it stays on the GPU; caches of all layers are handed over as a C
 from __future__ import annotations
 
 import ctypes
-from typing import Optional, Sequence, Tuple
+from typing import List, Optional, Sequence, Tuple
 
 import torch
 
@@ -32,9 +32,20 @@ def declare(lib: ctypes.CDLL) -> None:
         f.restype, f.argtypes = result, args
 
 
+def _places(addresses: Sequence[int], size: int) -> List[int]:
+    """The addresses of caches of `size` bytes, each once: a cache is worked on by the threads of one address, and those of
+    another would move rows of it under their hands."""
+    once = list(dict.fromkeys(addresses))
+    low = sorted(once)
+    if any(b - a < size for a, b in zip(low, low[1:])):
+        raise ValueError("optgqa: caches must not overlap in part")
+    return once
+
+
 class CacheSet:
     """K and V caches of all layers ([NB, Hkv, bs, D] each, all alike), and their addresses on the GPU: made once, where the
-    caches are (not under graph capture), and kept as long as they are."""
+    caches are (not under graph capture), and kept as long as they are.  One that several layers share may be there several
+    times and counts once; others must not overlap."""
 
     def __init__(self, caches: Sequence[torch.Tensor]):
         self.caches: Tuple[torch.Tensor, ...] = tuple(caches)
@@ -54,8 +65,9 @@ class CacheSet:
             if t.data_ptr() % 16:
                 raise ValueError(f"optgqa: cache {i} must lie on 16 bytes")
         self.shape, self.element_bytes, self.index = first.shape, first.element_size(), first.get_device()
-        self.pointers = torch.tensor([t.data_ptr() for t in self.caches], dtype=torch.int64, device=first.device)
-        self.count = len(self.caches)                            # (of addresses: what the kernels go by)
+        places = _places([t.data_ptr() for t in self.caches], first.numel() * first.element_size())
+        self.pointers = torch.tensor(places, dtype=torch.int64, device=first.device)
+        self.count = len(places)                                 # (of addresses: what the kernels go by)
 
 
 def _cache_set(caches) -> CacheSet:
