@@ -97,6 +97,12 @@ struct FastDiv {
     }
 };
 
+// a - b - less, rounded once, for any a and b (their difference can take 33 bits) and a small `less`.
+__host__ __device__ __forceinline__ float whole_difference(int a, int b, int less)
+{
+    return fmaf((float)((a >> 16) - (b >> 16)), 65536.f, (float)((a & 0xffff) - (b & 0xffff) - less));
+}
+
 // n / d for n >= 0 and d >= 1 whose quotient is below 2^20, given 1 / d to within an ulp or two: the product is off by less than
 // half then, the whole number below it by one at most, which the remainder tells.
 __host__ __device__ __forceinline__ int div_by_inverse(int n, int d, float d_inv)

@@ -425,10 +425,16 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
         const uint32_t hi = w + 1 < 0 ? 0xffffffffu : w + 1 < p.mask_words ? words[w + 1] : 0u;
         return __builtin_amdgcn_alignbit(hi, lo, (uint32_t)c0 & 31u) & there;
     };
+    // How far from the row's position `at` - `less` is.  (Exact near the row, however far along.  TREE: positions are the caller's, and two
+    // of them can be further apart than 32 bits say.)
+    auto away = [&](int at, int less = 0) __attribute__((always_inline)) {
+        if constexpr (TREE) return whole_difference(at, pos, less);
+        else return (float)(at - less - pos);
+    };
     // key0: the tile's first key
     auto softmax = [&](int key0, f32x16 st, auto masked) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(masked)::value;
-        const float b0 = fmaf(slope2, (float)(key0 + 4 * h2 - pos), -m_ref);         // (whole numbers' difference: exact near the row, however far)
+        const float b0 = fmaf(slope2, away(key0 + 4 * h2), -m_ref);
         float x[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -443,7 +449,7 @@ __device__ __forceinline__ void common_body(const CommonParams& p, const CommonJ
                 for (int e = 0; e < 16; ++e) {
                     const int in_tile = 8 * (e >> 2) + (e & 3), key = key0 + 4 * h2 + in_tile, c = key - job.pos0;
                     const int said = p.positions[job.tok0 + min(max(c, 0), last)];
-                    x[e] = fmaf(st[e], scale2, fmaf(slope2, (float)((c < 0 ? key : said) - in_tile - pos), -m_ref));
+                    x[e] = fmaf(st[e], scale2, fmaf(slope2, away(c < 0 ? key : said, in_tile), -m_ref));
                 }
             }
 #pragma unroll
