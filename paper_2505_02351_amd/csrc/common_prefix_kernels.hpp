@@ -164,10 +164,7 @@ template <bool TREE> struct OwnParts {
     __device__ __forceinline__ void number(int most, int& all)
     {
         pieces = div_by_inverse(steps + most - 1, most, __builtin_amdgcn_rcpf((float)most));
-        // TREE, no prefix: up to a share and a half, or four steps more than one, stay one piece, whose workgroup writes the output and leaves nothing to join.
-        // (64 trees of 16, 24 and 60 behind 1 000 - 2 000, 32 / 8 heads and 64 / 8: 101 -> 77 us, 133 -> 109, 380 -> 349.  Lines at 1.5, 2 and 2.5 shares: 64 of 12 - 24 behind
-        // 511 - 2 047 98, 104 and 99 us; 24 of 16 behind 1 000 - 2 000 52, 61 and 56, 32 of them 68, 59 and 55.)
-        if (TREE && alone && steps <= most + max(most >> 1, kTreeOneSteps - 1)) pieces = min(pieces, 1);
+        if (TREE && alone && tree_one_piece(steps, most)) pieces = min(pieces, 1);
         const int mine = pieces * segments, sum = lane_sums(mine);
         before = all + sum - mine;
         all += __builtin_amdgcn_readlane(sum, 63);

@@ -79,6 +79,16 @@ inline int64_t common_most_shares(int64_t cus, bool alone) { return std::max<int
 // 26.9 and 24.5.)
 constexpr int kTreeOneSteps = 5;
 
+// Trees with no prefix: a segment of up to a share and a half, or four steps more than one, stays one piece, whose workgroup writes the output and leaves
+// nothing to join.  (64 trees of 16 behind 1 000 - 2 000, 32 / 8 heads of 128, a line at one share 100 us, at a half more 86; of 24 130 and 117.  Lines at 1, 1.25, 2, 2.5 and 3
+// shares over 67 shapes of 4 to 128 trees, 4 to 64 tokens, contexts of 500 to 16 000, seven numbers of heads: 1.010, 1.015, 1.014, 1.021 and 1.044 times as long in
+// the geometric mean, single shapes 0.8 to 1.6 times: 32 trees of 16 behind 1 000 - 2 000 take 74 us, 59 with the line at 2.5; 18 of 12 behind 7 258, 40 / 8 heads of 64, 66
+// and 87.)
+__host__ __device__ __forceinline__ bool tree_one_piece(int steps, int share)
+{
+    return steps <= share + (share / 2 > kTreeOneSteps - 1 ? share / 2 : kTreeOneSteps - 1);
+}
+
 // Pieces that any call has that is no larger in its tokens, sequences, prefix, longest context and new tokens of a sequence: what is
 // held for a call serves all smaller ones.  (The pieces of the calls themselves go up and down: a workgroup's worth of rows more
 // means fewer ranges of the prefix.)
