@@ -62,8 +62,9 @@ class Server:
         self.masks = tree.masks.repeat(sequences, 1)
         self._prefill(prompt)
 
-    def resize(self, lens, slots=None, cu=None):
-        most = self.max_len if slots is None else slots.shape[0]
+    def resize(self, lens, slots=None, cu=None, most=None):
+        """most: tokens by which a sequence's length changes at most (a tree's, unless given)."""
+        most = self.tree.nodes if most is None else most
         G.resize_sequences(self.tables, self.lens, self.refs, lens, slots, cu, self.copies, self.counts, self.block, most, self.ws)
         if slots is not None:
             G.copy_blocks(self.caches, self.copies, self.counts)
@@ -96,7 +97,7 @@ class Server:
         cu = torch.full((self.B + 1,), n, dtype=torch.int32, device="cuda")
         cu[0] = 0
         slots = torch.empty(n, dtype=torch.int64, device="cuda")
-        self.resize(lens, slots, cu)
+        self.resize(lens, slots, cu, n)
         first, table, starts = lens[:1].clone(), self.tables[:1], cu[:2].clone()
         self._layers(prompt, torch.arange(n, device="cuda").int(), slots,
                      lambda out, q, k, v: G.paged_prefill(out, q, k, v, table, first, starts, None, self.scale, n))
