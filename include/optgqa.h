@@ -644,11 +644,11 @@ int optgqa_paged_attention_common_fp8_heads(void *out, const void *q, const void
  * away from it, new tokens positions[c] - positions[i]:
  *     s_j = scale * <q_i, K_g[j]> + alibi_slopes[h] * distance;   out_i = sum_j softmax(s)_j V_g[j]
  * A token that sees no key is +0.  With prefix_table empty (num_prefix_blocks 0) all of a sequence lies in its own blocks.  New
- * tokens that lie in the prefix are not seen.
+ * tokens that lie in the prefix are not seen.  There is no sliding window here (nor in optgqa_paged_attention_common).
  *
  *   tree_masks      [num_tokens][mask_words] uint32: token i's bit c is bit c % 32 of word c / 32; max_q_len at most 32 * mask_words.
  *                   Bits from n_b on are not looked at; optgqa_tree_masks_host makes masks from parents
- *   positions       [num_tokens] int32 (in a tree: base + depth); NULL is taken where alibi_slopes is
+ *   positions       [num_tokens] int32 (in a tree: base + depth; any values are taken); NULL is taken where alibi_slopes is
  *   workspace       optgqa_tree_workspace_bytes(...) bytes, which grow with each argument as optgqa_common_prefix_workspace_bytes does
  * All else - q, tables, lengths, slopes, 8-bit caches, what is not finite, bounds, errors - as optgqa_paged_attention_common.
  */

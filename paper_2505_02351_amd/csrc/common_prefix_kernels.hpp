@@ -25,9 +25,10 @@
 // TREE: the new tokens' keys are seen by masks, one bit for each of the sequence's new tokens, which tiles behind the context look up (two words of the row's
 // mask and a shift make a tile's 32 bits); everything in front of them is seen by all rows and needs none.  Without a prefix the own parts have the CUs to themselves, two
 // workgroups to each, and a segment that is one piece writes its output.  Bound by memory while rows are few (64 trees of 12 - 24 behind 511 - 2 047, 32 / 8 heads,
-// bf16, slopes: 90 - 98 us, 328 MB; 5.5 TB/s but for the pieces that end last), by matrix and vector instructions where they are many (two trees of 64 behind 32 000, 64 / 8,
-// bf16: 191 - 202 us, 670 - 710 TFLOP/s, over 1 000 with the weights' second half; 16 of 20 - 60 behind a common 8 192, 32 / 4, fp16, E4M3: 121 us, 820).
-// (head_dim 128 with bf16 takes all 256 registers that two workgroups to a CU leave a wave, and one more, which lies in scratch.)
+// bf16, slopes: 92 - 104 us, 328 MB; 5.5 TB/s but for the pieces that end last), by matrix and vector instructions where they are many (two trees of 64 behind 32 000, 64 / 8,
+// bf16: 191 - 203 us, 670 - 710 TFLOP/s, over 1 000 with the weights' second half; 16 of 20 - 60 behind a common 8 192, 32 / 4, fp16, E4M3: 121 - 133 us, 740 - 820).
+// (head_dim 128 with bf16 takes all 256 registers that two workgroups to a CU leave a wave, and one more, which lies in scratch; TREE 13 more over 2-byte caches, 10 over
+// 8-bit ones, around the tiles that a mask cuts.)
 #pragma once
 #include <type_traits>
 

@@ -69,8 +69,9 @@ inline int64_t tree_ranges(int64_t units, int64_t steps, int64_t slots, int64_t 
 }
 
 // Shares of all own parts: half a workgroup to a CU beside the prefix's; trees with no prefix have the CUs to themselves, two
-// workgroups to each, and with one as much of that as their steps are of all.  (1, 2, 3, 4 and 6 to a CU: two trees of 64 behind 32 000, 64 / 8 heads, the first launch alone, 323, 214, 222, 207 and 199 us; with the
-// join 206 at 2, 217 at 3, 212 at 4.  64 trees of 12 - 24 behind 511 - 2 047, 32 / 8, 110, 111 and 114 at 2, 3 and 4.)
+// workgroups to each, and with one as much of that as their steps are of all.  (1, 2, 3, 4 and 6 to a CU, replayed graphs with the join: two trees of 64 behind 32 000, 64 / 8 heads of
+// 128, bf16, 245, 199, 215, 205 and 216 us; 64 trees of 12 - 24 behind 511 - 2 047, 32 / 8, 106, 103, 108, 108 and 110; one of 16 behind 32 000 40, 41, 49, 52 and 61.  Behind a prefix of as
+// much again it varies: four of 40 - 64, 8 192 common and 6 000 - 8 000 own, 128, 135, 114, 112 and 121; eight of 16, 4 096 and 3 000 - 4 000, 50, 60, 57, 59 and 62.)
 inline int64_t common_most_shares(int64_t cus, bool alone) { return std::max<int64_t>(alone ? 2 * cus : cus / 2, 1); }
 
 // Trees with no prefix whose segments have so many steps at most are one piece each, whatever the shares; the call is one launch then, that writes the

@@ -75,9 +75,10 @@ struct KeepTokensParams {
 // Row start + paths[i] to row start + i.  Paths ascend, so paths[i] >= i: no row is written before it has been read for a later
 // place if, of any run of places, all are read before any is written; and a thread has one 16-byte column of all rows, so that
 // nobody else's order matters.
-// A head's row is 256 bytes somewhere in the caches, and that is what bounds it: 64 sequences, 249 tokens that move in 32 caches of 8 heads of 128 (33 MB),
-// 20 us, as long as a plain gather of such rows takes for half of the bytes (17).  Asking for all block numbers at once, three round
-// trips in place of five, changes nothing there, and costs 1.4 us where one small tree is all there is (2.8 us; 1.4).
+// What bounds it are round trips one after another, four to a row: its path, its two block numbers, itself.  `x` is set under conditions and lies in scratch
+// (144 bytes a lane), so that a row is waited for before the next one's path is asked for.  64 sequences, 249 tokens that move in 32 caches of 8 heads of 128
+// (33 MB): 19 us, 17 - 18 a pass among others, where 33 MB take 6.6.  (Asking for a run's block numbers at once, the rows still in scratch, changed nothing there and
+// cost 1.4 us where one small tree is all there is: 2.1 us.)
 constexpr int kKeepRun = 8;
 static __global__ __launch_bounds__(kPageThreads) void keep_tokens_kernel(const KeepTokensParams p)
 {
