@@ -758,7 +758,7 @@ int optgqa_verify_drafts(int64_t *tokens, int32_t *num_accepted, const void *tar
  * optgqa_fork_sequences: row i of tables_out [num_out][max_blocks_per_seq] and lens_out becomes row parents[i] of the old table, all of them
  * at once; a parent outside 0 .. num_seqs - 1: an empty row.  Blocks are shared; a sequence that is nobody's parent is
  * freed.  (Beams: parents as the search chose them.  Parallel samples: one parent several times.)  The new tables and lengths take
- * the old ones' place and must not overlap them (OPTGQA_ERR_SHAPE).
+ * the old ones' place and must not overlap them, the reference counts, the parents or each other (OPTGQA_ERR_SHAPE).
  *
  * optgqa_compact_blocks: of U blocks in use the i-th highest goes to the i-th lowest free one, as long as that is below U, at
  * most max_copies of them; tables and reference counts follow.  With max_copies >= num_blocks / 2 the blocks in use are

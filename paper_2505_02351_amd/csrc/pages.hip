@@ -99,12 +99,16 @@ int optgqa_fork_sequences(int32_t* tables_out, int32_t* lens_out, const int32_t*
     if (!ref_counts || (num_out && (!tables_out || !lens_out || !parents)) || (num_seqs && (!block_tables || !context_lens))) return OPTGQA_ERR_NULL;
     if (!aligned4({tables_out, lens_out, block_tables, context_lens, ref_counts, parents})) return OPTGQA_ERR_UNSUPPORTED;
     // (rows of the new table are written while others still read the old one)
-    auto apart = [](const int32_t* a, int64_t na, const int32_t* b, int64_t nb) {
-        return reinterpret_cast<uintptr_t>(a + na) <= reinterpret_cast<uintptr_t>(b) || reinterpret_cast<uintptr_t>(b + nb) <= reinterpret_cast<uintptr_t>(a);
+    struct Range { const int32_t* at; int64_t n; };
+    auto apart = [](const Range& a, const Range& b) {
+        const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.at), b0 = reinterpret_cast<uintptr_t>(b.at);
+        return a.n == 0 || b.n == 0 || a0 + 4 * (uint64_t)a.n <= b0 || b0 + 4 * (uint64_t)b.n <= a0;
     };
-    if (num_out && num_seqs && (!apart(tables_out, (int64_t)num_out * max_blocks_per_seq, block_tables, (int64_t)num_seqs * max_blocks_per_seq) ||
-                                !apart(lens_out, num_out, context_lens, num_seqs)))
-        return OPTGQA_ERR_SHAPE;
+    const Range rows{tables_out, (int64_t)num_out * max_blocks_per_seq}, lens{lens_out, num_out};
+    const Range others[] = {{block_tables, (int64_t)num_seqs * max_blocks_per_seq}, {context_lens, num_seqs}, {ref_counts, num_blocks}, {parents, num_out}};
+    bool all_apart = apart(rows, lens);
+    for (const Range& other : others) all_apart = all_apart && apart(rows, other) && apart(lens, other);
+    if (!all_apart) return OPTGQA_ERR_SHAPE;
     const ForkParams p{tables_out, lens_out, block_tables, context_lens, ref_counts, parents, num_out, num_seqs, max_blocks_per_seq, num_blocks,
                        __builtin_ctz(block_size)};
     return launch(fork_sequences_kernel, dim3(std::max(num_out, num_seqs), (unsigned)(((int64_t)max_blocks_per_seq + kForkEntries - 1) / kForkEntries)),
