@@ -282,7 +282,7 @@ __device__ __forceinline__ void resize_apply(const ResizeParams& p, const Resize
     if (from == 0 && (now <= old || enough)) p.context_lens[r] = now;
     if (!p.slots) return;
     const int begin = max(p.cu_new[r], 0), end = max(min(p.cu_new[r + 1], p.num_slots), 0);
-    // of the first tokens, where they fill a block (an entry that names none: they have no row, whatever the cache stores check)
+    // of the first tokens, where they fill a block (an entry that names none: they have no row, and the cache stores pass over slots below 0 alone)
     int kept = grows && have > 0 && (old >> shift) == have - 1 ? row[have - 1] : 0;
     if ((uint32_t)kept >= (uint32_t)p.num_blocks) kept = -1;
     const int grown = grows ? now - old : 0;                     // (lengths go up to 2^31 - 1, positions behind them would not)
